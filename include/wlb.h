@@ -1,11 +1,13 @@
 /*
  * wlb.h -- C ABI of the MI355X (gfx950) WLB-LLM hot path.
  *
- * Four groups of calls:
+ * Five groups of calls:
  *   wlb_pack        workload-aware variable-length packing (host, integers)
  *   wlb_shard*      context-parallel sharding maps          (host, integers)
  *   wlb_attn_plan   tile schedule for the attention kernels (device, integers)
  *   wlb_attn_fwd / wlb_attn_bwd   document-masked causal attention (device, bf16 MFMA)
+ *   wlb_embed_* / wlb_loss_*      the slots' rows of the vocabulary table, and the cross entropy of their next
+ *                                 tokens over the whole vocabulary, with the gradients of both (device)
  *
  * Conventions
  *   - Every call returns a wlb_status; WLB_OK is 0.  No exception crosses the
@@ -364,6 +366,74 @@ wlb_status wlb_attn_bwd(const wlb_attn_desc* desc, const void* q, const void* k,
                         const int32_t* q_idx, const int32_t* cu_seqlens_k,
                         void* dq, void* dk, void* dv,
                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * The two ends of the model on one context-parallel rank's slots: where the rows that attention works on
+ * come from, and what they are trained on.  Both are defined by the rank's sharding map (q_idx and
+ * cu_seqlens_k of wlb_shard) and the tokens of the packed sequence, both share one vocabulary table, and both are the part of a
+ * micro-batch's work that is linear in its tokens (W_l of Equation 2, Section 4.1).
+ *
+ *   tokens [t_kv]            int32: the packed sequence.  A value outside [0, vocab) is no word.
+ *   q_idx  [n_q]             int32: global token g of each slot; outside [0, t_kv): padding
+ *   table, dtable [vocab][hidden], x, dx [n_q][hidden]   bf16, 16-byte aligned
+ *
+ * Lookup:   x[i] = scale * table[tokens[g]], 0 for slots that are padding or hold no word.
+ * Loss:     the target of slot i is tokens[g + 1] if that token lies in the same document (cu_seqlens_k) and is a
+ *           word; a caller that does not train on some tokens (prompts) passes a copy of the sequence that has another
+ *           value there, -1 say.  With l[i][v] = scale * <x[i], table[v]>:
+ *           lse[i] = ln sum_v exp l[i][v],  loss[i] = lse[i] - l[i][target]  (float, natural logarithm).
+ *           A slot without a target has loss 0 and lse -inf, its row of x is never used, whatever it holds, and its row of dx is 0.
+ *           The logits are never kept: the forward leaves one maximum and one sum per slot and 256 words, the
+ *           backward computes them again for one piece of the vocabulary at a time.
+ *
+ * The gradients are those of sum_i d_loss[i] * loss[i] and of sum <dx, x>; dtable is THIS rank's partial sum (as dK / dV of
+ * the attention).  Sums are held in 32 bits and in an order that the sizes alone decide: deterministic, no
+ * floating-point atomics.  dx, dtable and x are rounded to bf16 once.  The softmax part of the logits' gradient enters
+ * its two matrix products in bf16, relative to the largest |d_loss|.
+ */
+typedef struct {
+    int32_t n_q;       /* local slots (rows of x), >= 1                                          */
+    int32_t t_kv;      /* tokens in the packed sequence, >= 1                                    */
+    int32_t n_docs;    /* documents; cu_seqlens_k has n_docs + 1 entries, last == t_kv           */
+    int32_t vocab;     /* rows of the table, 1 .. 2^30                                           */
+    int32_t hidden;    /* columns of the table, a multiple of 8, 8 .. 65536                      */
+    float   scale;     /* factor of the rows looked up, or of the logits: finite and > 0         */
+    int32_t flags;     /* WLB_VOCAB_* bits                                                       */
+} wlb_vocab_desc;
+
+enum {
+    /* wlb_embed_bwd adds to the dtable it finds instead of overwriting it: rows of words that no slot holds
+     * are left alone, the others become round(dtable + gradient).  For a table that is shared with the loss
+     * (wlb_loss_bwd first), or whose gradient is summed over micro-batches. */
+    WLB_VOCAB_ACCUMULATE = 1
+};
+
+/* Bytes of device workspace (256-byte aligned pointer expected) for wlb_embed_bwd, wlb_loss_fwd and wlb_loss_bwd.  Any
+ * output may be NULL.  Nothing in a workspace outlives a call: one buffer of the largest size serves all. */
+wlb_status wlb_vocab_workspace_size(const wlb_vocab_desc* desc, size_t* embed_bwd_bytes, size_t* loss_fwd_bytes,
+                                    size_t* loss_bwd_bytes);
+
+/* Lookup: x is overwritten.  flags must be 0.
+ * Errors of this and the following calls: INVALID_ARG (null or misaligned pointer, bad desc), UNSUPPORTED (hidden, vocab
+ * or sizes out of range), BUFFER_TOO_SMALL, HIP.  Argument errors are found before anything is enqueued. */
+wlb_status wlb_embed_fwd(const wlb_vocab_desc* desc, const int32_t* tokens, const int32_t* q_idx, const void* table,
+                         void* x, void* stream);
+
+/* Gradient of the lookup: dtable[v] = scale * sum of the rows dx[i] of the slots that hold word v, which are sorted by
+ * word (stable: summed in the order of the slots) in the workspace; rows of dx of other slots are never used. */
+wlb_status wlb_embed_bwd(const wlb_vocab_desc* desc, const int32_t* tokens, const int32_t* q_idx, const void* dx,
+                         void* dtable, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Loss: loss [n_q] and lse [n_q] are overwritten.  flags must be 0.  UNSUPPORTED also for x of 4 GiB or more. */
+wlb_status wlb_loss_fwd(const wlb_vocab_desc* desc, const void* x, const void* table, const int32_t* tokens,
+                        const int32_t* q_idx, const int32_t* cu_seqlens_k, float* loss, float* lse, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/* Gradients of the loss from the forward's lse and the gradient d_loss [n_q] of its losses (entries of slots without a
+ * target are never used): dx [n_q][hidden] and dtable [vocab][hidden] are overwritten.  flags must be 0. */
+wlb_status wlb_loss_bwd(const wlb_vocab_desc* desc, const void* x, const void* table, const int32_t* tokens,
+                        const int32_t* q_idx, const int32_t* cu_seqlens_k, const float* lse, const float* d_loss,
+                        void* dx, void* dtable, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------
  * Adaptive sharding selection (Section 5.3): predict the attention forward+backward latency of a

@@ -31,13 +31,15 @@ ATTN_NO_SHORT_PATH = 128
 ROW_FWD_TWO_HEADS = 1
 ROW_DQ_TWO_HEADS = 2
 ROW_SPAN = 4
+VOCAB_ACCUMULATE = 1
 
 STATUS_NAMES = {0: "WLB_OK", 1: "WLB_ERR_INVALID_ARG", 2: "WLB_ERR_BUFFER_TOO_SMALL",
                 3: "WLB_ERR_UNSUPPORTED", 4: "WLB_ERR_HIP"}
 
 EXPORTS = ["wlb_last_error", "wlb_pack", "wlb_pack_optimal", "wlb_packer_create", "wlb_packer_destroy", "wlb_packer_step",
            "wlb_packer_pending", "wlb_calib_mfma", "wlb_calib_atomic_add", "wlb_predict_latency", "wlb_select_sharding", "wlb_shard_size", "wlb_shard", "wlb_attn_workspace_size",
-           "wlb_attn_plan", "wlb_attn_plan_layout", "wlb_attn_plan_records", "wlb_attn_set_gang_weights", "wlb_attn_get_gang_weights", "wlb_attn_fwd", "wlb_attn_fwd_static", "wlb_attn_bwd"]
+           "wlb_attn_plan", "wlb_attn_plan_layout", "wlb_attn_plan_records", "wlb_attn_set_gang_weights", "wlb_attn_get_gang_weights", "wlb_attn_fwd", "wlb_attn_fwd_static", "wlb_attn_bwd",
+           "wlb_vocab_workspace_size", "wlb_embed_fwd", "wlb_embed_bwd", "wlb_loss_fwd", "wlb_loss_bwd"]
 
 
 class WlbError(RuntimeError):
@@ -50,6 +52,11 @@ class AttnDesc(C.Structure):
     _fields_ = [("n_q", C.c_int32), ("t_kv", C.c_int32), ("n_docs", C.c_int32), ("hq", C.c_int32),
                 ("hkv", C.c_int32), ("head_dim", C.c_int32), ("scale", C.c_float), ("flags", C.c_int32),
                 ("visible_pairs", C.c_int64)]
+
+
+class VocabDesc(C.Structure):
+    _fields_ = [("n_q", C.c_int32), ("t_kv", C.c_int32), ("n_docs", C.c_int32), ("vocab", C.c_int32), ("hidden", C.c_int32),
+                ("scale", C.c_float), ("flags", C.c_int32)]
 
 
 class PlanLayout(C.Structure):
@@ -418,6 +425,127 @@ class Attention:
         wlb_attn_bwd(desc, q, k, v, o, lse, d_o, self.q_idx, self.cu_k, dq, dk, dv, self.workspace)
         self.planned = True
         return dq, dk, dv
+
+
+# ------------------------------------------------------- lookup and loss over the vocabulary
+def vocab_desc(n_q, t_kv, n_docs, vocab, hidden, scale=1.0, flags=0) -> VocabDesc:
+    return VocabDesc(int(n_q), int(t_kv), int(n_docs), int(vocab), int(hidden), float(scale), int(flags))
+
+
+def wlb_vocab_workspace_size(desc: VocabDesc):
+    """-> bytes of workspace for (wlb_embed_bwd, wlb_loss_fwd, wlb_loss_bwd)"""
+    e, f, b = C.c_size_t(0), C.c_size_t(0), C.c_size_t(0)
+    _check(lib().wlb_vocab_workspace_size(C.byref(desc), C.byref(e), C.byref(f), C.byref(b)))
+    return e.value, f.value, b.value
+
+
+def _vocab_call(name, desc, tensors, workspace=None):
+    """One device call on the tensors' device and that device's current stream.  tensors: (tensor, dtype, shape) in the order of the C call."""
+    import torch
+    device = tensors[0][0].device
+    args = []
+    for t, dtype, shape in tensors:
+        args.append(_dev_ptr(t, dtype))
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name}: expected a tensor of shape {tuple(shape)}, got {tuple(t.shape)}")
+        if t.device != device:
+            raise ValueError(f"{name}: tensors on {device} and {t.device}")
+    if workspace is not None:
+        args += [_dev_ptr(workspace), C.c_size_t(workspace.numel() * workspace.element_size())]
+        if workspace.device != device:
+            raise ValueError(f"{name}: workspace on {workspace.device}, tensors on {device}")
+    with torch.cuda.device(device):
+        _check(getattr(lib(), name)(C.byref(desc), *args, _stream()))
+
+
+def wlb_embed_fwd(desc, tokens, q_idx, table, x):
+    import torch
+    i32, bf, d = torch.int32, torch.bfloat16, desc
+    _vocab_call("wlb_embed_fwd", d, [(tokens, i32, (d.t_kv,)), (q_idx, i32, (d.n_q,)), (table, bf, (d.vocab, d.hidden)), (x, bf, (d.n_q, d.hidden))])
+
+
+def wlb_embed_bwd(desc, tokens, q_idx, dx, dtable, workspace):
+    import torch
+    i32, bf, d = torch.int32, torch.bfloat16, desc
+    _vocab_call("wlb_embed_bwd", d, [(tokens, i32, (d.t_kv,)), (q_idx, i32, (d.n_q,)), (dx, bf, (d.n_q, d.hidden)), (dtable, bf, (d.vocab, d.hidden))], workspace)
+
+
+def wlb_loss_fwd(desc, x, table, tokens, q_idx, cu_seqlens_k, loss, lse, workspace):
+    import torch
+    i32, f32, bf, d = torch.int32, torch.float32, torch.bfloat16, desc
+    _vocab_call("wlb_loss_fwd", d, [(x, bf, (d.n_q, d.hidden)), (table, bf, (d.vocab, d.hidden)), (tokens, i32, (d.t_kv,)), (q_idx, i32, (d.n_q,)),
+                                    (cu_seqlens_k, i32, (d.n_docs + 1,)), (loss, f32, (d.n_q,)), (lse, f32, (d.n_q,))], workspace)
+
+
+def wlb_loss_bwd(desc, x, table, tokens, q_idx, cu_seqlens_k, lse, d_loss, dx, dtable, workspace):
+    import torch
+    i32, f32, bf, d = torch.int32, torch.float32, torch.bfloat16, desc
+    _vocab_call("wlb_loss_bwd", d, [(x, bf, (d.n_q, d.hidden)), (table, bf, (d.vocab, d.hidden)), (tokens, i32, (d.t_kv,)), (q_idx, i32, (d.n_q,)),
+                                    (cu_seqlens_k, i32, (d.n_docs + 1,)), (lse, f32, (d.n_q,)), (d_loss, f32, (d.n_q,)),
+                                    (dx, bf, (d.n_q, d.hidden)), (dtable, bf, (d.vocab, d.hidden))], workspace)
+
+
+class Vocabulary:
+    """The two ends of a model on one rank's slots (q_idx and cu_seqlens_k of wlb_shard): the slots' rows of the table and the
+    cross entropy of their next tokens, with gradients.  Owns the map on the device and a workspace for each kind of call,
+    allocated with the first (make one before capturing it into a graph) and kept: calls of one kind must be ordered on their
+    stream(s).  All arithmetic is in libwlb.  `tokens` are the packed sequence's [t_kv] int32; the loss takes a copy
+    with values outside [0, vocab) where a token is not trained on."""
+
+    def __init__(self, q_idx, cu_seqlens_k, vocab, hidden, embed_scale=1.0, logit_scale=1.0, device="cuda:0"):
+        import torch
+        self.torch = torch
+        self.device = torch.device(device)
+        self.q_idx = torch.as_tensor(np.ascontiguousarray(q_idx, dtype=np.int32)).to(self.device)
+        self.cu_k = torch.as_tensor(np.ascontiguousarray(cu_seqlens_k, dtype=np.int32)).to(self.device)
+        shape = (int(self.q_idx.numel()), int(cu_seqlens_k[-1]), int(self.cu_k.numel()) - 1, vocab, hidden)
+        self.embed_desc = vocab_desc(*shape, scale=embed_scale)
+        self.add_desc = vocab_desc(*shape, scale=embed_scale, flags=VOCAB_ACCUMULATE)
+        self.loss_desc = vocab_desc(*shape, scale=logit_scale)
+        self.workspace = {}
+
+    def _room(self, kind):
+        """The workspace of calls of a kind: 0 embed_backward, 1 loss, 2 loss_backward."""
+        if kind not in self.workspace:
+            nbytes = wlb_vocab_workspace_size(self.embed_desc)[kind]
+            self.workspace[kind] = self.torch.empty(nbytes, dtype=self.torch.uint8, device=self.device)
+        return self.workspace[kind]
+
+    def _empty(self, shape, dtype=None):
+        return self.torch.empty(shape, dtype=dtype or self.torch.bfloat16, device=self.device)
+
+    def embed(self, tokens, table, x=None):
+        """-> x [n_q][hidden]: embed_scale * table[token of the slot], 0 for padding"""
+        d = self.embed_desc
+        x = self._empty((d.n_q, d.hidden)) if x is None else x
+        wlb_embed_fwd(d, tokens, self.q_idx, table, x)
+        return x
+
+    def embed_backward(self, tokens, dx, dtable=None, accumulate=False):
+        """-> dtable [vocab][hidden], overwritten, or added to (accumulate)"""
+        d = self.add_desc if accumulate else self.embed_desc
+        if dtable is None:
+            if accumulate:
+                raise ValueError("embed_backward: accumulate needs the dtable to add to")
+            dtable = self._empty((d.vocab, d.hidden))
+        wlb_embed_bwd(d, tokens, self.q_idx, dx, dtable, self._room(0))
+        return dtable
+
+    def loss(self, x, table, tokens, loss=None, lse=None):
+        """-> (loss [n_q], lse [n_q]) in float: 0 and -inf for slots without a target"""
+        d = self.loss_desc
+        loss = self._empty((d.n_q,), self.torch.float32) if loss is None else loss
+        lse = self._empty((d.n_q,), self.torch.float32) if lse is None else lse
+        wlb_loss_fwd(d, x, table, tokens, self.q_idx, self.cu_k, loss, lse, self._room(1))
+        return loss, lse
+
+    def loss_backward(self, x, table, tokens, lse, d_loss, dx=None, dtable=None):
+        """-> (dx [n_q][hidden], dtable [vocab][hidden]), both overwritten"""
+        d = self.loss_desc
+        dx = self._empty((d.n_q, d.hidden)) if dx is None else dx
+        dtable = self._empty((d.vocab, d.hidden)) if dtable is None else dtable
+        wlb_loss_bwd(d, x, table, tokens, self.q_idx, self.cu_k, lse, d_loss, dx, dtable, self._room(2))
+        return dx, dtable
 
 
 def wlb_attn_set_gang_weights(kernel: int, weights=None):
