@@ -20,8 +20,10 @@ struct GemmShape {
     static constexpr bool MP = MP_, MQ = MQ_;                            // operand kinds: m / n contiguous in memory
     static constexpr int TM = WM * BM * 32, TN = WN * BN * 32;
     static constexpr int P_BYTES = TM * kStepK * 2, Q_BYTES = TN * kStepK * 2, STAGE = P_BYTES + Q_BYTES;
-    static constexpr int OUT_BYTES = 4 * 8192;                           // 8 KiB of a wavefront's output on its way to memory
-    static constexpr int LDS_BYTES = 2 * STAGE > OUT_BYTES ? 2 * STAGE : OUT_BYTES;
+    // Five LDS slots of one operand's tile, or two buffers of both tiles
+    static constexpr bool RING = P_BYTES == 32768 && Q_BYTES == 32768;
+    static constexpr int LDS_BYTES = RING ? 5 * P_BYTES : 2 * STAGE;
+    static_assert(LDS_BYTES >= 4 * 8192, "8 KiB of each wavefront's output on its way to memory");
     static_assert(WM * WN == 4, "four wavefronts");
 };
 
@@ -97,9 +99,9 @@ struct Fragments {
             for (int kk = 0; kk < 4; ++kk) at[kk] = tile + row * 128 + swz<8>(row, 2 * kk + lane / 32) * 16;
         }
     }
-    __device__ __forceinline__ void flip(int stage_bytes) {
+    __device__ __forceinline__ void move(int bytes) {
 #pragma unroll
-        for (int i = 0; i < (M ? B : 4); ++i) at[i] += stage_bytes;
+        for (int i = 0; i < (M ? B : 4); ++i) at[i] += bytes;
     }
     // read r of READS of 16-step kk into f
     __device__ __forceinline__ void read(int r, int kk, bf16x8 (&f)[B]) const {
@@ -154,6 +156,10 @@ struct Gemm {
         constexpr int NP = decltype(cp)::N, NQ = decltype(cq)::N;
         Fragments<S::TM, BM, S::MP> fp;
         Fragments<S::TN, BN, S::MQ> fq;
+        if constexpr (S::RING) {
+            ring(cp, cq, fp, fq, steps, tail);
+            return;
+        }
         fp.init(lds, wm * BM, lane);
         fq.init(lds + S::P_BYTES, wn * BN, lane);
 #pragma unroll
@@ -187,8 +193,8 @@ struct Gemm {
                     cp.seek(s + 2, steps);
                     cq.seek(s + 2, steps);
                     const int flip = (s & 1) ? -S::STAGE : S::STAGE;
-                    fp.flip(flip);
-                    fq.flip(flip);
+                    fp.move(flip);
+                    fq.move(flip);
                 }
 #pragma unroll
                 for (int x = 0; x < BM * BN || x < RP + RQ || (kk == 3 && x < NP + NQ); ++x) {
@@ -203,6 +209,71 @@ struct Gemm {
                         const int i = x / BN, j = x % BN;
                         acc[i][j] = mfma32(a[kk & 1][i], b[kk & 1][j], acc[i][j]);
                     }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+        wait_lds();
+        wait_vmem();
+        __syncthreads();
+    }
+
+    // The steps of a wide tile.  The operands' tiles P0 Q0 P1 Q1 .. go to five LDS slots in turn.  Copies take half of the time that the
+    // vector memory path has (64 KiB of 128 a step), so they are spread over the step: four wavefronts that
+    // issued all of them in one quarter of it waited for each other (72 % of the time).  Step s copies P of s + 2 beside its first three
+    // 16-steps, into the slot that Q of s - 1 left, and behind the step's barrier Q of s + 2 into the slot of its own P.
+    template <class CP, class CQ, class FP, class FQ>
+    __device__ __forceinline__ void ring(CP& cp, CQ& cq, FP& fp, FQ& fq, int steps, int tail) {
+        constexpr int BM = S::BM, BN = S::BN, NP = CP::N, NQ = CQ::N, SLOT = S::P_BYTES, RP = FP::READS, RQ = FQ::READS;
+        static_assert(NP == 8 && NQ == 8 && BM * BN == 16, "where in a step the copies stand");
+        fp.init(lds, wm * BM, lane);
+        fq.init(lds + SLOT, wn * BN, lane);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            if (s == steps - 1 && tail) { cp.cut(tail, wave, lane); cq.cut(tail, wave, lane); }
+            cp.seek(s, steps);
+            cq.seek(s, steps);
+#pragma unroll
+            for (int n = 0; n < NP; ++n) cp.issue(n, lds + 2 * s * SLOT, wave);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) cq.issue(n, lds + (2 * s + 1) * SLOT, wave);
+        }
+        bf16x8 a[2][BM], b[2][BN];
+        wait_vmem_le<NP + NQ>();
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < RP; ++r) fp.read(r, 0, a[0]);
+#pragma unroll
+        for (int r = 0; r < RQ; ++r) fq.read(r, 0, b[0]);
+        int p_slot = 0, q_slot = 1;             // of this step's tiles
+        for (int s = 0; s < steps; ++s) {
+            if (s + 2 == steps - 1 && tail) cp.cut(tail, wave, lane);
+            cp.seek(s + 2, steps);
+            const uint32_t to_p = lds + (p_slot == 0 ? 4 : p_slot - 1) * SLOT, to_q = lds + p_slot * SLOT;
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+                if (kk == 3) {
+                    // the step's last operands are in registers and the next step's tiles in LDS, for every wavefront
+                    wait_lds();
+                    wait_vmem_le<NP>();
+                    __syncthreads();
+                    if (s + 2 == steps - 1 && tail) cq.cut(tail, wave, lane);
+                    cq.seek(s + 2, steps);
+                    const int p_move = p_slot < 3 ? 2 : -3, q_move = q_slot < 3 ? 2 : -3;
+                    fp.move(p_move * SLOT);
+                    fq.move(q_move * SLOT);
+                    p_slot += p_move;
+                    q_slot += q_move;
+                }
+#pragma unroll
+                for (int x = 0; x < 16; ++x) {
+                    // reads of the operands of the next 16-step, copies, MFMAs of this one
+                    if (x < RQ) fq.read(x, (kk + 1) & 3, b[(kk + 1) & 1]);
+                    else if (x < RP + RQ) fp.read(x - RQ, (kk + 1) & 3, a[(kk + 1) & 1]);
+                    if (kk == 3 && x % 2 == 1) cq.issue(x / 2, to_q, wave);
+                    if (kk < 3 && (kk * 16 + x) % 6 == 2) cp.issue((kk * 16 + x) / 6, to_p, wave);
+                    const int i = x / BN, j = x % BN;
+                    acc[i][j] = mfma32(a[kk & 1][i], b[kk & 1][j], acc[i][j]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
