@@ -1,11 +1,14 @@
-// Matrix product of a workgroup: D[m][n] = sum_k P[m][k] * Q[n][k], bf16 operands, fp32 sums, for the loss over the vocabulary.
+// Matrix products of the loss over the vocabulary: D[m][n] = sum_k P[m][k] * Q[n][k], bf16 operands, fp32 sums.
 //
 // Four wavefronts, each WM-th x WN-th part of a tile of TM x TN.  Operands move global -> LDS by buffer_load ... lds in
-// steps of 64 along k, double buffered, and LDS -> registers one 16-step ahead of the MFMAs.  An operand lies in memory either with k
+// steps of 64 along k, and LDS -> registers one 16-step ahead of the MFMAs.  An operand lies in memory either with k
 // contiguous (rows of m or n: "K") or with m or n contiguous (rows of k: "M"); the second kind is read from LDS with transpose reads, so
-// no operand is ever written transposed.  Wide tiles take one workgroup to a compute unit and one wavefront to a SIMD: a wavefront's
-// 128 x 128 part needs 8 KiB of LDS reads for 16 MFMAs (8192 flops a byte), half of what 8 wavefronts of 128 x 64 would read.
+// no operand is ever written transposed.  Wide tiles (256 x 256) take one workgroup to a compute unit and one wavefront to a SIMD: a wavefront's
+// 128 x 128 part needs 8 KiB of LDS reads for 16 MFMAs, half of what 8 wavefronts of 128 x 64 would read.  They are bound by the MFMA rate at
+// the clock that the power limit leaves (1.5 - 1.8 GHz).  Narrow tiles (few slots) are bound by the table's bytes.
 #pragma once
+#include <type_traits>
+
 #include "wlb_device.h"
 
 namespace wlb {
@@ -23,8 +26,71 @@ struct GemmShape {
     // Five LDS slots of one operand's tile, or two buffers of both tiles
     static constexpr bool RING = P_BYTES == 32768 && Q_BYTES == 32768;
     static constexpr int LDS_BYTES = RING ? 5 * P_BYTES : 2 * STAGE;
-    static_assert(LDS_BYTES >= 4 * 8192, "8 KiB of each wavefront's output on its way to memory");
+    static constexpr int PER_CU = LDS_BYTES > 81920 ? 1 : 2;             // workgroups to a compute unit
     static_assert(WM * WN == 4, "four wavefronts");
+    static_assert(LDS_BYTES >= 4 * 8192, "8 KiB of each wavefront's output on its way to memory");
+};
+
+// A piece of work of a workgroup: a tile, and which part of k.
+struct GemmItem {
+    int tm, tn;
+    int k0, depth;              // first k and how many (0: the product is 0)
+    int part;                   // -1: the whole sum, else where its fp32 partial sum goes
+};
+
+// Distribution of the tiles of an ntm x ntn grid over the launch.  Whole tiles go round after round to the workgroups; those of a last round that would not
+// fill the launch are divided along k, so that all workgroups share them, and leave partial sums that a second launch joins.  Workgroup b runs on
+// XCD b % 8; each XCD takes a consecutive share of the tiles in bands of kBand tiles along n, so that the workgroups that run side by
+// side on it share kBand operand tiles along n and a few along m in its L2.
+constexpr int kBand = 8, kMaxParts = 128;
+struct GemmGrid {
+    int ntm, ntn, depth, workgroups, whole, left, parts;
+    // part_steps: a divided tile's part has at least this many steps
+    __device__ __forceinline__ GemmGrid(int ntm_, int ntn_, int depth_, int workgroups_, int part_steps) : ntm(ntm_), ntn(ntn_), depth(depth_), workgroups(workgroups_) {
+        const int tiles = ntm * ntn, steps = (depth + kStepK - 1) / kStepK;
+        left = uniform(tiles % workgroups);
+        parts = left ? uniform(workgroups / left) : 1;
+        if (parts > kMaxParts) parts = kMaxParts;
+        if (parts > steps / part_steps) parts = steps / part_steps;
+        if (parts < 2) { parts = 1; left = 0; }
+        whole = tiles - left;
+    }
+    __device__ __forceinline__ void place(int t, GemmItem& it) const {
+        const int band = t / (kBand * ntm), high = min(kBand, ntn - band * kBand);
+        t -= band * kBand * ntm;
+        const int tm = t / high;
+        it.tm = uniform(tm);            // divisions leave scalars in vector registers
+        it.tn = uniform(band * kBand + (t - tm * high));
+    }
+    // item `round` of workgroup b; false: there is none
+    __device__ __forceinline__ bool item(int b, int round, GemmItem& it) const {
+        it.tm = it.tn = 0;
+        const int x = b % kLists, i = b / kLists, side = workgroups / kLists;
+        const int per = (whole + kLists - 1) / kLists, mine = round * side + i, t = x * per + mine;
+        it.k0 = 0; it.depth = depth; it.part = -1;
+        const int rounds = (per + side - 1) / side;
+        if (round < rounds) {
+            if (mine < per && t < whole) { place(t, it); return true; }
+            if (round < rounds - 1 || left == 0) return false;
+            round = rounds;                          // no whole tile in the last round
+        }
+        const int u = x * side + i;
+        if (left == 0 || round > rounds || u >= left * parts) return false;
+        const int part = u / left, steps = (depth + kStepK - 1) / kStepK;
+        place(whole + u - part * left, it);
+        const int s0 = (int)((long long)steps * part / parts), s1 = (int)((long long)steps * (part + 1) / parts);
+        it.k0 = uniform(s0 * kStepK);
+        it.depth = uniform(min(depth, s1 * kStepK) - s0 * kStepK);
+        it.part = uniform((u - part * left) * parts + part);
+        return true;
+    }
+};
+
+// An operand's part of a tile, as the caller gives it.
+struct GemmOperand {
+    const void* at;             // first element of the tile at the first k
+    int valid;                  // rows or columns of the tile that exist
+    const int32_t* list;        // kind K: numbers of the rows counted from `at`, or null
 };
 
 // Copies of one operand's tile.  T: its width (rows of kind K, columns of kind M).
@@ -37,47 +103,50 @@ struct TileCopy {
     int voff[N];
     BufRsrc rs;
     uint64_t base;
-    uint32_t step_bytes;
+    uint32_t row_bytes;
+    int wave, lane, left;                                       // k that exist from this step's start on
 
-    static __device__ __forceinline__ int row_of(int wave, int n, int lane) { return (wave * N + n) * RPI + lane / CH; }
-    static __device__ __forceinline__ int chunk_of(int row, int lane) {
-        return M ? (lane % CH) ^ ((row & 3) << 2) : swz<8>(row, lane % 8);
+    __device__ __forceinline__ int row_of(int n) const { return (wave * N + n) * RPI + lane / CH; }
+    __device__ __forceinline__ int chunk_of(int n) const { return M ? (lane % CH) ^ ((row_of(n) & 3) << 2) : swz<8>(row_of(n), lane % 8); }
+    // ld: elements between rows
+    __device__ __forceinline__ void init(long long ld, int wave_, int lane_) {
+        row_bytes = (uint32_t)(ld * 2);
+        wave = wave_;
+        lane = lane_;
     }
-    // base: the tile's first element at k = 0; ld: elements between rows; valid: rows (K) or columns (M, rounded up to 8 by what lies there) inside the operand;
-    // list: the rows' numbers (K), rows counted from `base`, or null
-    __device__ __forceinline__ void init(const void* at, long long ld, int valid, const int32_t* list, int wave, int lane) {
-        base = (uint64_t)(uintptr_t)at;
-        step_bytes = M ? (uint32_t)(kStepK * ld * 2) : kStepK * 2;
+    __device__ __forceinline__ void tile(const GemmOperand& o) {
+        base = (uint64_t)(uintptr_t)o.at;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const int row = row_of(wave, n, lane), chunk = chunk_of(row, lane);
-            if (M) {
-                voff[n] = chunk * 8 < valid ? (int)((uint32_t)row * (uint32_t)(ld * 2) + chunk * 16) : kOutOfRange;
-            } else {
-                const uint32_t from = row < valid ? (list ? (uint32_t)list[row] : (uint32_t)row) : 0u;
-                voff[n] = row < valid ? (int)(from * (uint32_t)(ld * 2) + chunk * 16) : kOutOfRange;
-            }
+            const int row = row_of(n), chunk = chunk_of(n);
+            const bool on = (M ? chunk * 8 : row) < o.valid;
+            uint32_t from = (uint32_t)row;
+            if (!M && o.list) from = on ? (uint32_t)o.list[row] : 0u;
+            voff[n] = on ? (int)(from * row_bytes + chunk * 16) : kOutOfRange;
         }
     }
-    // lanes whose k lies at or beyond `left` (k counted from the step's start): zeros from here on
-    __device__ __forceinline__ void cut(int left, int wave, int lane) {
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const int row = row_of(wave, n, lane), chunk = chunk_of(row, lane);
-            if ((M ? row : chunk * 8) >= left) voff[n] = kOutOfRange;
-        }
-    }
-    // the descriptor of step s; steps past the last one load nothing
-    __device__ __forceinline__ void seek(int s, int steps) {
-        const uint64_t a = base + (uint64_t)s * step_bytes;
-        rs.r[0] = (int)(uint32_t)a;
-        rs.r[1] = (int)(uint32_t)((a >> 32) & 0xffffu);
-        rs.r[2] = s < steps ? (int)kMaxRecords : 0;
+    // the tile's first step, of `depth` along k; on = false: nothing is loaded
+    __device__ __forceinline__ void first(int depth, bool on) {
+        rs.r[0] = uniform((int)(uint32_t)base);
+        rs.r[1] = uniform((int)(uint32_t)((base >> 32) & 0xffffu));
+        rs.r[2] = on ? (int)kMaxRecords : 0;
         rs.r[3] = 0x00020000;
+        left = depth;
     }
-    __device__ __forceinline__ void issue(int n, uint32_t lds_tile, int wave) const {
-        dma_issue_1k(rs.r, lds_tile + (uint32_t)(wave * N + n) * 1024u, voff[n], 0u);
+    __device__ __forceinline__ void next() {
+        const uint64_t a = (((uint64_t)(uint32_t)rs.r[1] << 32) | (uint32_t)rs.r[0]) + (uint64_t)(M ? kStepK * row_bytes : kStepK * 2u);
+        rs.r[0] = (int)(uint32_t)a;
+        rs.r[1] = (int)(uint32_t)(a >> 32);
+        left -= kStepK;
     }
+    // in the last step of a tile: lanes whose k does not exist load zeros from here on
+    __device__ __forceinline__ void cut() {
+        if (left >= kStepK) return;
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            if ((M ? row_of(n) : chunk_of(n) * 8) >= left) voff[n] = kOutOfRange;
+    }
+    __device__ __forceinline__ void issue(int n, uint32_t lds_tile) const { dma_issue_1k(rs.r, lds_tile + (uint32_t)(wave * N + n) * 1024u, voff[n], 0u); }
 };
 
 // Operand fragments of a wavefront out of LDS: B blocks of 32 rows (columns).
@@ -116,127 +185,144 @@ struct Fragments {
     }
 };
 
-// An operand as the caller gives it (the tile's own part of it).
-struct GemmOperand {
-    const void* at;             // first element of the tile at the first k
-    long long ld;               // elements between rows
-    int valid;                  // rows or columns of the tile that exist
-    const int32_t* list;        // kind K: numbers of the rows, or null
-};
-
+// Work is a GemmGrid with, for an item, operands p(item) and q(item) and leading dimensions ldp, ldq.  done(gemm, item, ahead, lds) takes the sums of an
+// item; lds: 32 KiB, 8 of them each wavefront's own; ahead: what done.load(gemm, item) returned in front of the item's steps (loads that would hold up its end).
 template <class S>
 struct Gemm {
     f32x16 acc[S::BM][S::BN];   // register r of lane l: m = 32 i + (r/4)*8 + (l/32)*4 + r%4, n = 32 j + l%32 of the wavefront's part
     int wave, lane, wm, wn;
     uint32_t lds;
+    TileCopy<S::TM, S::MP> cp;
+    TileCopy<S::TN, S::MQ> cq;
+    Fragments<S::TM, S::BM, S::MP> fp;
+    Fragments<S::TN, S::BN, S::MQ> fq;
+    static constexpr int NP = decltype(cp)::N, NQ = decltype(cq)::N, RP = decltype(fp)::READS, RQ = decltype(fq)::READS;
 
-    __device__ __forceinline__ void start(char* smem) {
+    static __device__ __forceinline__ int steps_of(const GemmItem& it, int least) { return max((it.depth + kStepK - 1) / kStepK, least); }
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < S::BM; ++i)
+#pragma unroll
+            for (int j = 0; j < S::BN; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    }
+
+    template <class Work, class Done>
+    __device__ __forceinline__ void run(char* smem, const Work& work, const Done& done) {
         wave = uniform((int)threadIdx.x >> 6);
         lane = threadIdx.x & 63;
         wm = wave % S::WM;
         wn = wave / S::WM;
         lds = (uint32_t)(uintptr_t)smem;
+        cp.init(work.ldp, wave, lane);
+        cq.init(work.ldq, wave, lane);
+        if constexpr (S::RING) ring(work, done);
+        else pair(work, done);
     }
 
-    // acc = the product over k of [0, depth).  Ends with every copy landed and LDS free for other use.
-    __device__ __forceinline__ void run(const GemmOperand& p, const GemmOperand& q, int depth) {
+    // One item at a time in two LDS buffers: narrow tiles, of which two workgroups share a compute unit.
+    template <class Work, class Done>
+    __device__ __forceinline__ void pair(const Work& work, const Done& done) {
         constexpr int BM = S::BM, BN = S::BN;
+        GemmItem it;
+        for (int round = 0; work.item((int)blockIdx.x, round, it); ++round) {
+            const int steps = steps_of(it, 1);
+            const auto ahead = done.load(*this, it);
+            clear();
+            cp.tile(work.p(it));
+            cq.tile(work.q(it));
+            fp.init(lds, wm * BM, lane);
+            fq.init(lds + S::P_BYTES, wn * BN, lane);
 #pragma unroll
-        for (int i = 0; i < BM; ++i)
+            for (int s = 0; s < 2; ++s) {
+                if (s) { cp.next(); cq.next(); }
+                else { cp.first(it.depth, true); cq.first(it.depth, true); }
+                cp.cut();
+                cq.cut();
 #pragma unroll
-            for (int j = 0; j < BN; ++j)
+                for (int n = 0; n < NP; ++n) cp.issue(n, lds + s * S::STAGE);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-        const int steps = (depth + kStepK - 1) / kStepK, tail = depth % kStepK;
-        if (steps == 0) return;
-        TileCopy<S::TM, S::MP> cp;
-        TileCopy<S::TN, S::MQ> cq;
-        cp.init(p.at, p.ld, p.valid, p.list, wave, lane);
-        cq.init(q.at, q.ld, q.valid, q.list, wave, lane);
-        constexpr int NP = decltype(cp)::N, NQ = decltype(cq)::N;
-        Fragments<S::TM, BM, S::MP> fp;
-        Fragments<S::TN, BN, S::MQ> fq;
-        if constexpr (S::RING) {
-            ring(cp, cq, fp, fq, steps, tail);
-            return;
-        }
-        fp.init(lds, wm * BM, lane);
-        fq.init(lds + S::P_BYTES, wn * BN, lane);
+                for (int n = 0; n < NQ; ++n) cq.issue(n, lds + s * S::STAGE + S::P_BYTES);
+            }
+            bf16x8 a[2][BM], b[2][BN];
+            wait_vmem_le<NP + NQ>();
+            __syncthreads();
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            if (s == steps - 1 && tail) { cp.cut(tail, wave, lane); cq.cut(tail, wave, lane); }
-            cp.seek(s, steps);
-            cq.seek(s, steps);
+            for (int r = 0; r < RP; ++r) fp.read(r, 0, a[0]);
 #pragma unroll
-            for (int n = 0; n < NP; ++n) cp.issue(n, lds + s * S::STAGE, wave);
+            for (int r = 0; r < RQ; ++r) fq.read(r, 0, b[0]);
+            for (int s = 0; s < steps; ++s) {
+                const uint32_t stage = lds + (s & 1) * S::STAGE;
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) cq.issue(n, lds + s * S::STAGE + S::P_BYTES, wave);
-        }
-        bf16x8 a[2][BM], b[2][BN];
-        wait_vmem_le<NP + NQ>();
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < decltype(fp)::READS; ++r) fp.read(r, 0, a[0]);
-#pragma unroll
-        for (int r = 0; r < decltype(fq)::READS; ++r) fq.read(r, 0, b[0]);
-        for (int s = 0; s < steps; ++s) {
-            const uint32_t stage = lds + (s & 1) * S::STAGE;
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {
-                constexpr int RP = decltype(fp)::READS, RQ = decltype(fq)::READS;
-                if (kk == 3) {
-                    // the step's last operands are in registers and the next step's tiles in LDS, for every wavefront
-                    wait_lds();
-                    wait_vmem();
-                    __syncthreads();
-                    if (s + 2 == steps - 1 && tail) { cp.cut(tail, wave, lane); cq.cut(tail, wave, lane); }
-                    cp.seek(s + 2, steps);
-                    cq.seek(s + 2, steps);
-                    const int flip = (s & 1) ? -S::STAGE : S::STAGE;
-                    fp.move(flip);
-                    fq.move(flip);
-                }
-#pragma unroll
-                for (int x = 0; x < BM * BN || x < RP + RQ || (kk == 3 && x < NP + NQ); ++x) {
-                    // reads of the operands of the next 16-step, copies of the step after the next, MFMAs of this one
-                    if (x < RQ) fq.read(x, (kk + 1) & 3, b[(kk + 1) & 1]);
-                    else if (x < RP + RQ) fp.read(x - RQ, (kk + 1) & 3, a[(kk + 1) & 1]);
+                for (int kk = 0; kk < 4; ++kk) {
                     if (kk == 3) {
-                        if (x < NP) cp.issue(x, stage, wave);
-                        else if (x < NP + NQ) cq.issue(x - NP, stage + S::P_BYTES, wave);
+                        // the step's last operands are in registers and the next step's tiles in LDS, for every wavefront
+                        wait_lds();
+                        wait_vmem();
+                        __syncthreads();
+                        cp.next();
+                        cq.next();
+                        cp.cut();
+                        cq.cut();
+                        const int flip = (s & 1) ? -S::STAGE : S::STAGE;
+                        fp.move(flip);
+                        fq.move(flip);
                     }
-                    if (x < BM * BN) {
-                        const int i = x / BN, j = x % BN;
-                        acc[i][j] = mfma32(a[kk & 1][i], b[kk & 1][j], acc[i][j]);
+#pragma unroll
+                    for (int x = 0; x < BM * BN || x < RP + RQ || (kk == 3 && x < NP + NQ); ++x) {
+                        // reads of the operands of the next 16-step, copies of the step after the next, MFMAs of this one
+                        if (x < RQ) fq.read(x, (kk + 1) & 3, b[(kk + 1) & 1]);
+                        else if (x < RP + RQ) fp.read(x - RQ, (kk + 1) & 3, a[(kk + 1) & 1]);
+                        if (kk == 3) {
+                            if (x < NP) cp.issue(x, stage);
+                            else if (x < NP + NQ) cq.issue(x - NP, stage + S::P_BYTES);
+                        }
+                        if (x < BM * BN) {
+                            const int i = x / BN, j = x % BN;
+                            acc[i][j] = mfma32(a[kk & 1][i], b[kk & 1][j], acc[i][j]);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
                     }
-                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
+            wait_lds();
+            wait_vmem();
+            __syncthreads();
+            done(*this, it, ahead, lds);
+            wait_lds();
+            __syncthreads();
         }
-        wait_lds();
-        wait_vmem();
-        __syncthreads();
     }
 
-    // The steps of a wide tile.  The operands' tiles P0 Q0 P1 Q1 .. go to five LDS slots in turn.  Copies take half of the time that the
-    // vector memory path has (64 KiB of 128 a step), so they are spread over the step: four wavefronts that
+    // Wide tiles.  The operands' tiles P0 Q0 P1 Q1 .. go to five LDS slots in turn, and on without a break from one item to the next:
+    // while an item's sums go to memory, the first two steps of the next are in LDS or on their way, and the slot that is left holds the output.  Copies
+    // take half of the time that the vector memory path has (64 KiB of 128 a step), so they are spread over the step: four wavefronts that
     // issued all of them in one quarter of it waited for each other (72 % of the time).  Step s copies P of s + 2 beside its first three
-    // 16-steps, into the slot that Q of s - 1 left, and behind the step's barrier Q of s + 2 into the slot of its own P.
-    template <class CP, class CQ, class FP, class FQ>
-    __device__ __forceinline__ void ring(CP& cp, CQ& cq, FP& fp, FQ& fq, int steps, int tail) {
-        constexpr int BM = S::BM, BN = S::BN, NP = CP::N, NQ = CQ::N, SLOT = S::P_BYTES, RP = FP::READS, RQ = FQ::READS;
-        static_assert(NP == 8 && NQ == 8 && BM * BN == 16, "where in a step the copies stand");
+    // 16-steps, into the slot that Q of s - 1 left, and behind the step's barrier Q of s + 2 into the slot of its own P.  An item has two steps
+    // at least (the second may be zeros), so that the steps two ahead of its last two are the next item's first two.
+    template <class Work, class Done>
+    __device__ __forceinline__ void ring(const Work& work, const Done& done) {
+        constexpr int BM = S::BM, BN = S::BN, SLOT = S::P_BYTES;
+        static_assert(NP == 8 && NQ == 8 && BM * BN == 16 && RP + RQ <= 16, "where in a step the copies stand");
+        GemmItem it, next;
+        if (!work.item((int)blockIdx.x, 0, it)) return;
+        cp.tile(work.p(it));
+        cq.tile(work.q(it));
+        cp.first(it.depth, true);
+        cq.first(it.depth, true);
         fp.init(lds, wm * BM, lane);
         fq.init(lds + SLOT, wn * BN, lane);
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            if (s == steps - 1 && tail) { cp.cut(tail, wave, lane); cq.cut(tail, wave, lane); }
-            cp.seek(s, steps);
-            cq.seek(s, steps);
+            if (s) { cp.next(); cq.next(); }
+            cp.cut();
+            cq.cut();
 #pragma unroll
-            for (int n = 0; n < NP; ++n) cp.issue(n, lds + 2 * s * SLOT, wave);
+            for (int n = 0; n < NP; ++n) cp.issue(n, lds + 2 * s * SLOT);
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) cq.issue(n, lds + (2 * s + 1) * SLOT, wave);
+            for (int n = 0; n < NQ; ++n) cq.issue(n, lds + (2 * s + 1) * SLOT);
         }
         bf16x8 a[2][BM], b[2][BN];
         wait_vmem_le<NP + NQ>();
@@ -245,53 +331,93 @@ struct Gemm {
         for (int r = 0; r < RP; ++r) fp.read(r, 0, a[0]);
 #pragma unroll
         for (int r = 0; r < RQ; ++r) fq.read(r, 0, b[0]);
+        f32x16 zeros;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) zeros[r] = 0.f;
         int p_slot = 0, q_slot = 1;             // of this step's tiles
-        for (int s = 0; s < steps; ++s) {
-            if (s + 2 == steps - 1 && tail) cp.cut(tail, wave, lane);
-            cp.seek(s + 2, steps);
-            const uint32_t to_p = lds + (p_slot == 0 ? 4 : p_slot - 1) * SLOT, to_q = lds + p_slot * SLOT;
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {
-                if (kk == 3) {
-                    // the step's last operands are in registers and the next step's tiles in LDS, for every wavefront
-                    wait_lds();
-                    wait_vmem_le<NP>();
-                    __syncthreads();
-                    if (s + 2 == steps - 1 && tail) cq.cut(tail, wave, lane);
-                    cq.seek(s + 2, steps);
-                    const int p_move = p_slot < 3 ? 2 : -3, q_move = q_slot < 3 ? 2 : -3;
-                    fp.move(p_move * SLOT);
-                    fq.move(q_move * SLOT);
-                    p_slot += p_move;
-                    q_slot += q_move;
+        for (int round = 1;; ++round) {
+            const int steps = steps_of(it, 2);
+            const bool more = work.item((int)blockIdx.x, round, next);
+            const auto ahead = done.load(*this, it);
+            GemmOperand next_p = {}, next_q = {};
+            if (more) { next_p = work.p(next); next_q = work.q(next); }
+            auto step = [&](int s, auto fresh) __attribute__((always_inline)) {       // fresh: the sums start here
+                if (s + 2 == steps) {
+                    if (more) cp.tile(next_p);
+                    cp.first(next.depth, more);
+                } else {
+                    cp.next();
                 }
+                cp.cut();
+                const uint32_t to_p = lds + (p_slot == 0 ? 4 : p_slot - 1) * SLOT, to_q = lds + p_slot * SLOT;
 #pragma unroll
-                for (int x = 0; x < 16; ++x) {
-                    // reads of the operands of the next 16-step, copies, MFMAs of this one
-                    if (x < RQ) fq.read(x, (kk + 1) & 3, b[(kk + 1) & 1]);
-                    else if (x < RP + RQ) fp.read(x - RQ, (kk + 1) & 3, a[(kk + 1) & 1]);
-                    if (kk == 3 && x % 2 == 1) cq.issue(x / 2, to_q, wave);
-                    if (kk < 3 && (kk * 16 + x) % 6 == 2) cp.issue((kk * 16 + x) / 6, to_p, wave);
-                    const int i = x / BN, j = x % BN;
-                    acc[i][j] = mfma32(a[kk & 1][i], b[kk & 1][j], acc[i][j]);
-                    __builtin_amdgcn_sched_barrier(0);
+                for (int kk = 0; kk < 4; ++kk) {
+                    if (kk == 3) {
+                        // the step's last operands are in registers and the next step's tiles in LDS, for every wavefront
+                        wait_lds();
+                        wait_vmem_le<NP>();
+                        __syncthreads();
+                        if (s + 2 == steps) {
+                            if (more) cq.tile(next_q);
+                            cq.first(next.depth, more);
+                        } else {
+                            cq.next();
+                        }
+                        cq.cut();
+                        const int p_move = p_slot < 3 ? 2 : -3, q_move = q_slot < 3 ? 2 : -3;
+                        fp.move(p_move * SLOT);
+                        fq.move(q_move * SLOT);
+                        p_slot += p_move;
+                        q_slot += q_move;
+                    }
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        // reads of the operands of the next 16-step, copies, MFMAs of this one
+                        if (x < RQ) fq.read(x, (kk + 1) & 3, b[(kk + 1) & 1]);
+                        else if (x < RP + RQ) fp.read(x - RQ, (kk + 1) & 3, a[(kk + 1) & 1]);
+                        if (kk == 3 && x % 2 == 1) cq.issue(x / 2, to_q);
+                        if (kk < 3 && (kk * 16 + x) % 6 == 2) cp.issue((kk * 16 + x) / 6, to_p);
+                        const int i = x / BN, j = x % BN;
+                        acc[i][j] = mfma32(a[kk & 1][i], b[kk & 1][j], fresh && kk == 0 ? zeros : acc[i][j]);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
-            }
+            };
+            step(0, std::true_type{});
+            for (int s = 1; s < steps; ++s) step(s, std::false_type{});
+            // the next P goes to the slot used here: each wavefront's copies to the 8 KiB that are its own
+            sums_ready();
+            done(*this, it, ahead, lds + (p_slot == 0 ? 4 : p_slot - 1) * SLOT);
+            wait_lds();
+            if (!more) break;
+            it = next;
         }
-        wait_lds();
         wait_vmem();
-        __syncthreads();
     }
 
-    // Rows of output through LDS, so that memory sees whole 256-byte pieces: the wavefront's columns n of block j, `Bytes` = 2 (bf16: all
-    // of the wavefront's 32 BM values of a row, 4 blocks at most) or 4 (fp32: two blocks at a time).  value(i, j, r) gives the values; put(n, m, ptr) takes
-    // 16 bytes: n, m counted in the tile.  The caller's LDS must be free; each wavefront uses a part of its own.
+    // A sum.  Wide tiles' lie in accumulation registers, which vector instructions cannot read: moving them one by one, by hand, keeps the compiler from
+    // copying them all.  It does not see when they were written: sums_ready() comes first.
+    __device__ __forceinline__ float sum(int i, int j, int r) const {
+        if constexpr (!S::RING) return acc[i][j][r];
+        float v;
+        asm("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(acc[i][j][r]));
+        return v;
+    }
+    __device__ __forceinline__ void sums_ready() const {
+        if constexpr (!S::RING) return;
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");       // an MFMA's result: 19 wait states
+        __builtin_amdgcn_sched_barrier(0);
+    }
+
+    // Rows of output through LDS, so that memory sees whole 256-byte pieces: `Bytes` = 2 (bf16: all of the wavefront's 32 BM values of a row)
+    // or 4 (fp32: two blocks at a time).  value(i, j, r) gives the values; put(n, m, bits) takes 16 bytes: n, m counted in the tile.
     template <int Bytes, class V, class Put>
-    __device__ __forceinline__ void rows_out(V value, Put put) {
+    __device__ __forceinline__ void rows_out(uint32_t room, V value, Put put) {
         constexpr int G = Bytes == 2 ? (S::BM < 4 ? S::BM : 4) : (S::BM < 2 ? S::BM : 2);        // blocks of 32 m at a time
         constexpr int ROWB = G * 32 * Bytes, CH = ROWB / 16, RPI = 64 / CH;                      // bytes, chunks of a row; rows per pass
         static_assert(S::BM % G == 0 && ROWB <= 256, "8 KiB of a wavefront");
-        const uint32_t mine = lds + wave * 8192;
+        const uint32_t mine = room + wave * 8192;
 #pragma unroll
         for (int j = 0; j < S::BN; ++j)
 #pragma unroll
@@ -306,6 +432,7 @@ struct Gemm {
                         const float v0 = value(i0 + i, j, r), v1 = value(i0 + i, j, r + 1), v2 = value(i0 + i, j, r + 2), v3 = value(i0 + i, j, r + 3);
                         if (Bytes == 2) *reinterpret_cast<WLB_LDS bf16x4*>((uintptr_t)to) = pack4(v0, v1, v2, v3);
                         else *reinterpret_cast<WLB_LDS f32x4*>((uintptr_t)to) = f32x4{v0, v1, v2, v3};
+                        if (r == 12) __builtin_amdgcn_sched_barrier(0);         // few values out of the accumulators at a time
                     }
                 wait_lds();
                 __builtin_amdgcn_wave_barrier();
@@ -318,6 +445,12 @@ struct Gemm {
                 wait_lds();
                 __builtin_amdgcn_wave_barrier();
             }
+    }
+
+    // the partial sums of a divided tile: [TN][256] floats
+    __device__ __forceinline__ void part_out(uint32_t room, float* to) {
+        rows_out<4>(room, [&](int i, int j, int r) __attribute__((always_inline)) { return sum(i, j, r); },
+                    [&](int n, int m, const i32x4& v) __attribute__((always_inline)) { *reinterpret_cast<i32x4*>(to + n * S::TM + m) = v; });
     }
 };
 

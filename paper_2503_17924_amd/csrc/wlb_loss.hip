@@ -12,6 +12,7 @@
 // rows; by the table's bytes below that.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "wlb_gemm.h"
 #include "wlb_vocab.h"
@@ -129,125 +130,228 @@ __global__ void __launch_bounds__(kRowsThreads) loss_rows_kernel(RowsArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------
-// Workgroup -> tile of an ntm x ntn grid.  Workgroup b runs on XCD b % 8; each XCD takes a consecutive share of the tiles in bands of
-// kBand tiles along n, so that the workgroups that run side by side on it share kBand operand tiles along n and a few along m in its L2.
-constexpr int kBand = 8;
-__device__ __forceinline__ bool find_tile(int ntm, int ntn, int layers, int& tm, int& tn, int& layer) {
-    const int plane = ntm * ntn, all = plane * layers, per = (all + kLists - 1) / kLists, i = (int)blockIdx.x / kLists;
-    int t = ((int)blockIdx.x % kLists) * per + i;
-    if (i >= per || t >= all) return false;
-    layer = t / plane;
-    t -= layer * plane;
-    const int band = t / (kBand * ntm), high = min(kBand, ntn - band * kBand);
-    t -= band * kBand * ntm;
-    tm = t / high;
-    tn = band * kBand + t % high;
-    return true;
+// Products and their work lists.  A wide tile is divided along k (GemmGrid) only into parts of kWideParts steps and more: its partial sums cost a write
+// and a read of 256 KiB and a launch (20 us in all, what 14 steps take).  Narrow ones, which few slots leave to a few workgroups, from kNarrowParts on for dX,
+// else never.
+constexpr int kWideParts = 16, kNarrowParts = 4, kNever = 1 << 30;
+
+struct Work : GemmGrid {
+    const __bf16 *p_at, *q_at;
+    long long ldp, ldq;
+    int pm, qn;                      // rows or columns of the operands
+    const int32_t* list;             // rows of q, or null
+    int tile_m, tile_n;
+    bool p_down, q_down;             // operand kind M: k runs down the rows
+    template <class S>
+    static __device__ __forceinline__ Work make(const __bf16* p, long long ldp, int pm, const __bf16* q, long long ldq, int qn, const int32_t* list, int depth,
+                                                int workgroups, int narrow_parts) {
+        Work w(GemmGrid((pm + S::TM - 1) / S::TM, (qn + S::TN - 1) / S::TN, depth, workgroups, S::RING ? kWideParts : narrow_parts));
+        w.p_at = p; w.q_at = q; w.ldp = ldp; w.ldq = ldq; w.pm = pm; w.qn = qn; w.list = list;
+        w.tile_m = S::TM; w.tile_n = S::TN; w.p_down = S::MP; w.q_down = S::MQ;
+        return w;
+    }
+    __device__ __forceinline__ explicit Work(const GemmGrid& g) : GemmGrid(g) {}
+    __device__ __forceinline__ GemmOperand p(const GemmItem& i) const {
+        const int m0 = i.tm * tile_m;
+        return GemmOperand{p_down ? p_at + (long long)i.k0 * ldp + m0 : p_at + (long long)m0 * ldp + i.k0, pm - m0, nullptr};
+    }
+    __device__ __forceinline__ GemmOperand q(const GemmItem& i) const {
+        const int n0 = i.tn * tile_n;
+        if (list) return GemmOperand{q_at + i.k0, qn - n0, list + n0};
+        return GemmOperand{q_down ? q_at + (long long)i.k0 * ldq + n0 : q_at + (long long)n0 * ldq + i.k0, qn - n0, nullptr};
+    }
+};
+
+// Joins the parts of divided tiles in order: f(tm, tn, n, m, four sums), a wavefront to a row n of a tile.
+template <class S, class F>
+__device__ __forceinline__ void join_parts(const Work& w, const float* parts, F f) {
+    static_assert(S::TM == 256, "four columns a lane");
+    const int lane = threadIdx.x & 63, id = uniform((int)blockIdx.x * 4 + ((int)threadIdx.x >> 6));
+    GemmItem it;
+    if (id >= w.left * S::TN) return;
+    w.place(w.whole + id / S::TN, it);
+    const int n = id % S::TN;
+    const f32x4* from = reinterpret_cast<const f32x4*>(parts + ((size_t)(id / S::TN) * w.parts * S::TN + n) * S::TM) + lane;
+    f32x4 sum = {0, 0, 0, 0};
+    constexpr int kAhead = 8;
+    for (int k = 0; k < w.parts; k += kAhead) {
+        f32x4 v[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) v[i] = from[(size_t)min(k + i, w.parts - 1) * (S::TN * S::TM / 4)];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (k + i < w.parts) sum += v[i];
+    }
+    f(it.tm, it.tn, n, lane * 4, sum);
 }
-static unsigned tile_grid(long long tiles) { return (unsigned)((tiles + kLists - 1) / kLists * kLists); }
 
 // ------------------------------------------------------------------------------------------
+// Forward.  Exponents are in units of log2, relative to a tile's reference: its largest l times c2, rounded.  What the rounding
+// is off by cancels, since the reference is what the sum is stored with.
 struct StatsArgs {
     const __bf16 *x, *table;
     const int32_t *rows, *target, *count;
-    float2* part;                    // [word tiles][pitch]: maximum of l and sum of exp(c (l - maximum)) of a row in a tile
-    float* target_logit;             // [labelled]
-    int vocab, hidden, pitch;
+    float2* part;                    // [word tiles][pitch]: reference r of a row in a tile, and sum of 2^(c2 l - r)
+    float* target_logit;             // [labelled] l of the target
+    float* parts;                    // divided tiles
+    int vocab, hidden, pitch, workgroups;
     float c2;                        // scale * log2(e)
 };
 
 template <class S>
-__global__ void __launch_bounds__(256, S::LDS_BYTES > 81920 ? 1 : 2) loss_stats_kernel(StatsArgs a) {
-    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
+__device__ __forceinline__ Work stats_work(const StatsArgs& a) {
     const int n_rows = ld_const(a.count);
-    int tm, tn, unused;
-    if (!find_tile((a.vocab + S::TM - 1) / S::TM, (n_rows + S::TN - 1) / S::TN, 1, tm, tn, unused)) return;
-    const int m0 = tm * S::TM, n0 = tn * S::TN;
-    Gemm<S> g;
-    g.start(smem);
-    g.run(GemmOperand{a.table + (size_t)m0 * a.hidden, a.hidden, a.vocab - m0, nullptr}, GemmOperand{a.x, a.hidden, n_rows - n0, a.rows + n0}, a.hidden);
-    const int first = m0 + g.wm * (S::BM * 32) + (g.lane / 32) * 4;       // word of register 0 of block 0
-    if (m0 + S::TM > a.vocab) {
+    return Work::make<S>(a.table, a.hidden, a.vocab, a.x, a.hidden, n_rows, a.rows, a.hidden, a.workgroups, kNever);
+}
+
+template <class S>
+struct StatsDone {
+    const StatsArgs& a;
+    const Work& w;
+    char* smem;
+    struct Ahead { int target[S::BN]; };        // of the lane's rows, -1: no row
+    __device__ __forceinline__ Ahead load(const Gemm<S>& g, const GemmItem& it) const {
+        Ahead h;
 #pragma unroll
-        for (int i = 0; i < S::BM; ++i)
-#pragma unroll
-            for (int j = 0; j < S::BN; ++j)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (first + i * 32 + (r / 4) * 8 + r % 4 >= a.vocab) g.acc[i][j][r] = -INFINITY;
+        for (int j = 0; j < S::BN; ++j) {
+            const int row = it.tn * S::TN + g.wn * (S::BN * 32) + j * 32 + g.lane % 32;
+            h.target[j] = row < w.qn ? a.target[row] : -1;
+        }
+        return h;
     }
-    float2* s_part = (float2*)smem;                                       // [WM][TN]
-#pragma unroll
-    for (int j = 0; j < S::BN; ++j) {
-        const int n = g.wn * (S::BN * 32) + j * 32 + g.lane % 32;
-        const int t = n0 + n < n_rows ? a.target[n0 + n] - first : -1;    // register that holds the target, if this lane has it
-        float most = -INFINITY, at_target = 0.f;
-        bool mine = false;
-#pragma unroll
-        for (int i = 0; i < S::BM; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) most = fmaxf(most, g.acc[i][j][r]);
-        most = fmaxf(most, xhalf(most));
-        if (__any(t >= 0 && t < S::BM * 32)) {
+    __device__ __forceinline__ void operator()(Gemm<S>& g, const GemmItem& it, const Ahead& ahead, uint32_t room) const {
+        if (it.part >= 0) {
+            g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN));
+            return;
+        }
+        const int m0 = it.tm * S::TM, n0 = it.tn * S::TN, n_rows = w.qn;
+        const int first = m0 + g.wm * (S::BM * 32) + (g.lane / 32) * 4;       // word of register 0 of block 0
+        float2* s_part = (float2*)(smem + (room - g.lds));                    // [WM][TN]
+        auto block = [&](int j, auto edge) __attribute__((always_inline)) {   // edge: words of the tile lie past the end
+            const int n = g.wn * (S::BN * 32) + j * 32 + g.lane % 32;
+            auto logit = [&](int i, int r) __attribute__((always_inline)) {
+                const float l = g.sum(i, j, r);
+                return edge && first + i * 32 + (r / 4) * 8 + r % 4 >= a.vocab ? -INFINITY : l;
+            };
+            const int t = ahead.target[j] < 0 ? -1 : ahead.target[j] - first;    // register that holds the target, if this lane has it
+            float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
             for (int i = 0; i < S::BM; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (t == i * 32 + (r / 4) * 8 + r % 4) { mine = true; at_target = g.acc[i][j][r]; }
-            if (mine) a.target_logit[n0 + n] = at_target;
+                for (int r = 0; r < 16; ++r) most[r % 4] = fmaxf(most[r % 4], logit(i, r));
+            float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+            top = fmaxf(top, xhalf(top));
+            if (__any(t >= 0 && t < S::BM * 32)) {
+#pragma unroll
+                for (int i = 0; i < S::BM; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (t == i * 32 + (r / 4) * 8 + r % 4) a.target_logit[n0 + n] = g.sum(i, j, r);
+            }
+            const float ref = top == -INFINITY ? -INFINITY : top * a.c2, from = top == -INFINITY ? 0.f : ref;    // a wavefront all of whose words lie past the end
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < S::BM; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum[r % 4] += fast_exp2(__builtin_fmaf(logit(i, r), a.c2, -from));
+            float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            all += xhalf(all);
+            if (g.lane < 32) s_part[g.wm * S::TN + n] = float2{ref, all};
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        if (m0 + S::TM > a.vocab) {
+#pragma unroll
+            for (int j = 0; j < S::BN; ++j) block(j, std::true_type{});
+        } else {
+#pragma unroll
+            for (int j = 0; j < S::BN; ++j) block(j, std::false_type{});
         }
-        const float ref = most == -INFINITY ? 0.f : most;                 // a wavefront all of whose words lie past the end
+        __syncthreads();
+        for (int n = threadIdx.x; n < S::TN; n += 256) {
+            if (n0 + n >= n_rows) continue;
+            float ref = s_part[n].x, sum = 0.f;
+#pragma unroll
+            for (int k = 1; k < S::WM; ++k) ref = fmaxf(ref, s_part[k * S::TN + n].x);
+#pragma unroll
+            for (int k = 0; k < S::WM; ++k) {
+                const float2 p = s_part[k * S::TN + n];
+                sum += p.x == -INFINITY ? p.y : p.y * fast_exp2(p.x - ref);      // p.y is 0 where every word lies past the end, or NaN
+            }
+            a.part[(size_t)it.tm * a.pitch + n0 + n] = float2{ref, sum};
+        }
+        __syncthreads();
+    }
+};
+
+template <class S>
+__global__ void __launch_bounds__(256, S::PER_CU) loss_stats_kernel(StatsArgs a) {
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
+    const Work w = stats_work<S>(a);
+    Gemm<S> gemm;
+    gemm.run(smem, w, StatsDone<S>{a, w, smem});
+}
+
+// The same for a row of a divided tile.
+template <class S>
+__global__ void __launch_bounds__(256) loss_stats_parts_kernel(StatsArgs a) {
+    const Work w = stats_work<S>(a);
+    join_parts<S>(w, a.parts, [&](int tm, int tn, int n, int m, const f32x4& l) __attribute__((always_inline)) {
+        const int row = tn * S::TN + n, word = tm * S::TM + m;
+        if (row >= w.qn) return;
+        float most = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) most = word + k < a.vocab ? fmaxf(most, l[k]) : most;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+        const float ref = most == -INFINITY ? -INFINITY : most * a.c2, from = most == -INFINITY ? 0.f : ref;
+        const int t = a.target[row] - word;
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < S::BM; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) sum += fast_exp2((g.acc[i][j][r] - ref) * a.c2);
-        sum += xhalf(sum);
-        if (g.lane < 32) s_part[g.wm * S::TN + n] = float2{most, sum};
-    }
-    __syncthreads();
-    for (int n = threadIdx.x; n < S::TN; n += 256) {
-        if (n0 + n >= n_rows) continue;
-        float most = s_part[n].x, sum = 0.f;
-#pragma unroll
-        for (int w = 1; w < S::WM; ++w) most = fmaxf(most, s_part[w * S::TN + n].x);
-#pragma unroll
-        for (int w = 0; w < S::WM; ++w) {
-            const float2 p = s_part[w * S::TN + n];
-            sum += p.x == -INFINITY ? p.y : p.y * fast_exp2((p.x - most) * a.c2);      // p.y is 0 where every word lies past the end, or NaN
+        for (int k = 0; k < 4; ++k) {
+            if (word + k < a.vocab) sum += fast_exp2(__builtin_fmaf(l[k], a.c2, -from));
+            if (t == k) a.target_logit[row] = l[k];
         }
-        a.part[(size_t)tm * a.pitch + n0 + n] = float2{most, sum};
-    }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+        if ((threadIdx.x & 63) == 0) a.part[(size_t)tm * a.pitch + row] = float2{ref, sum};
+    });
 }
 
 // A slot's tiles combined: 32 rows to a workgroup, 8 threads to a row.
 __global__ void __launch_bounds__(256) loss_join_kernel(const float2* part, const float* target_logit, const int32_t* rows, const int32_t* count, float* loss,
-                                                        float* lse, int tiles, int pitch, float scale) {
+                                                        float* lse, int tiles, int pitch, float c2) {
     __shared__ float2 s_part[8][32];
     const int n_rows = *count, x = threadIdx.x & 31, y = threadIdx.x >> 5, row = (int)blockIdx.x * 32 + x;
-    const float c2 = scale * kLog2e;
+    constexpr float kLn2 = 0.6931471805599453f;
     if ((int)blockIdx.x * 32 >= n_rows) return;
-    float most = -INFINITY, sum = 0.f;
+    constexpr int kAhead = 8;
+    float ref = -INFINITY, sum = 0.f;
     if (row < n_rows)
-        for (int t = y; t < tiles; t += 8) {
-            const float2 p = part[(size_t)t * pitch + row];
-            const float m = fmaxf(most, p.x);
-            sum = (most == -INFINITY ? sum : sum * fast_exp2((most - m) * c2)) + (p.x == -INFINITY ? p.y : p.y * fast_exp2((p.x - m) * c2));
-            most = m;
+        for (int t = y; t < tiles; t += 8 * kAhead) {
+            float2 p[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) p[k] = t + 8 * k < tiles ? part[(size_t)(t + 8 * k) * pitch + row] : float2{-INFINITY, 0.f};
+            float r = ref;
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) r = fmaxf(r, p[k].x);
+            sum = ref == -INFINITY ? sum : sum * fast_exp2(ref - r);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) sum += p[k].x == -INFINITY ? p[k].y : p[k].y * fast_exp2(p[k].x - r);
+            ref = r;
         }
-    s_part[y][x] = float2{most, sum};
+    s_part[y][x] = float2{ref, sum};
     __syncthreads();
     if (y != 0 || row >= n_rows) return;
-    for (int w = 1; w < 8; ++w) most = fmaxf(most, s_part[w][x].x);
+    for (int k = 1; k < 8; ++k) ref = fmaxf(ref, s_part[k][x].x);
     sum = 0.f;
-    for (int w = 0; w < 8; ++w) {
-        const float2 p = s_part[w][x];
-        sum += p.x == -INFINITY ? p.y : p.y * fast_exp2((p.x - most) * c2);
+    for (int k = 0; k < 8; ++k) {
+        const float2 p = s_part[k][x];
+        sum += p.x == -INFINITY ? p.y : p.y * fast_exp2(p.x - ref);
     }
-    const float ln = logf(sum);
+    const float log_sum = log2f(sum);
     const int slot = rows[row];
-    lse[slot] = scale * most + ln;
-    loss[slot] = scale * (most - target_logit[row]) + ln;
+    lse[slot] = kLn2 * (ref + log_sum);
+    loss[slot] = kLn2 * (log_sum - __builtin_fmaf(target_logit[row], c2, -ref));
 }
 
 // ------------------------------------------------------------------------------------------
@@ -269,113 +373,184 @@ struct GradArgs {
     __bf16 *rows_x;                  // [labelled][hidden]
     __bf16 *d;                       // [labelled][pitch]: D of the piece
     __bf16 *dx, *dtable;
-    float *part;                     // [splits][n_q][hidden]: dX so far
+    float *dx_sum;                   // [n_q][hidden]: dX of the pieces so far, where there are several
+    float *parts;                    // divided tiles
     const int32_t *rows, *target, *count;
     const float *row_lse, *row_weight, *factor;
-    int vocab, hidden, n_q, pitch;
+    int vocab, hidden, n_q, pitch, workgroups;
     int piece0, piece_n;             // words of the piece
-    int splits;                      // of the piece along the words, for dX
-    int add, final;                  // dX: there are earlier pieces; this piece is the last and not split
+    int add, final;                  // dX: there are earlier pieces; this piece is the last
     float c2;
 };
 
 template <class S>
-__global__ void __launch_bounds__(256, S::LDS_BYTES > 81920 ? 1 : 2) loss_d_kernel(GradArgs a) {
+__device__ __forceinline__ Work d_work(const GradArgs& a) {
+    return Work::make<S>(a.table + (size_t)a.piece0 * a.hidden, a.hidden, a.piece_n, a.rows_x, a.hidden, ld_const(a.count), nullptr, a.hidden, a.workgroups, kNever);
+}
+
+template <class S>
+struct DDone {
+    const GradArgs& a;
+    const Work& w;
+    struct Ahead { float lse[S::BN], weight[S::BN]; int target[S::BN]; };       // of the lane's rows
+    __device__ __forceinline__ Ahead load(const Gemm<S>& g, const GemmItem& it) const {
+        Ahead h;
+#pragma unroll
+        for (int j = 0; j < S::BN; ++j) {
+            const int row = it.tn * S::TN + g.wn * (S::BN * 32) + j * 32 + g.lane % 32;
+            const bool on = row < w.qn;
+            h.lse[j] = on ? a.row_lse[row] : 0.f;
+            h.weight[j] = on ? a.row_weight[row] : 0.f;
+            h.target[j] = on ? a.target[row] : -1;
+        }
+        return h;
+    }
+    __device__ __forceinline__ void operator()(Gemm<S>& g, const GemmItem& it, const Ahead& h, uint32_t room) const {
+        if (it.part >= 0) {
+            g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN));
+            return;
+        }
+        const int m0 = it.tm * S::TM, n0 = it.tn * S::TN;
+        const int first = m0 + g.wm * (S::BM * 32) + (g.lane / 32) * 4;     // word of register 0 of block 0, in the piece
+        auto out = [&](auto edge) __attribute__((always_inline)) {          // edge: words of the tile lie past the end, D is 0 there
+            g.template rows_out<2>(
+                room,
+                [&](int i, int j, int r) __attribute__((always_inline)) {
+                    const int word = i * 32 + (r / 4) * 8 + r % 4;
+                    const float e = fast_exp2(__builtin_fmaf(g.sum(i, j, r), a.c2, -h.lse[j] * kLog2e)), p = edge && first + word >= a.piece_n ? 0.f : e;
+                    return h.weight[j] * (h.target[j] - a.piece0 - first == word ? p - 1.f : p);
+                },
+                [&](int n, int m, const i32x4& v) __attribute__((always_inline)) {
+                    if (n0 + n < w.qn) *reinterpret_cast<i32x4*>(a.d + (size_t)(n0 + n) * a.pitch + m0 + m) = v;
+                });
+        };
+        if (m0 + S::TM > a.piece_n) out(std::true_type{});
+        else out(std::false_type{});
+    }
+};
+
+template <class S>
+__global__ void __launch_bounds__(256, S::PER_CU) loss_d_kernel(GradArgs a) {
     __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
-    const int n_rows = ld_const(a.count);
-    int tm, tn, unused;
-    if (!find_tile((a.piece_n + S::TM - 1) / S::TM, (n_rows + S::TN - 1) / S::TN, 1, tm, tn, unused)) return;
-    const int m0 = tm * S::TM, n0 = tn * S::TN, v0 = a.piece0 + m0;
-    Gemm<S> g;
-    g.start(smem);
-    g.run(GemmOperand{a.table + (size_t)v0 * a.hidden, a.hidden, a.vocab - v0, nullptr},
-          GemmOperand{a.rows_x + (size_t)n0 * a.hidden, a.hidden, n_rows - n0, nullptr}, a.hidden);
-    const int first = v0 + g.wm * (S::BM * 32) + (g.lane / 32) * 4;
-    if (v0 + S::TM > a.vocab) {                     // words past the end: D is 0
+    const Work w = d_work<S>(a);
+    Gemm<S> gemm;
+    gemm.run(smem, w, DDone<S>{a, w});
+}
+
+template <class S>
+__global__ void __launch_bounds__(256) loss_d_parts_kernel(GradArgs a) {
+    const Work w = d_work<S>(a);
+    join_parts<S>(w, a.parts, [&](int tm, int tn, int n, int m, const f32x4& l) __attribute__((always_inline)) {
+        const int row = tn * S::TN + n, word = tm * S::TM + m;
+        if (row >= w.qn) return;
+        const float lse2 = a.row_lse[row] * kLog2e, weight = a.row_weight[row];
+        const int t = a.target[row] - a.piece0 - word;
+        float d[4];
 #pragma unroll
-        for (int i = 0; i < S::BM; ++i)
-#pragma unroll
-            for (int j = 0; j < S::BN; ++j)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (first + i * 32 + (r / 4) * 8 + r % 4 >= a.vocab) g.acc[i][j][r] = -INFINITY;
-    }
-    float lse2[S::BN], weight[S::BN];
-    int target[S::BN];
-#pragma unroll
-    for (int j = 0; j < S::BN; ++j) {
-        const int n = n0 + g.wn * (S::BN * 32) + j * 32 + g.lane % 32;
-        const bool on = n < n_rows;
-        lse2[j] = on ? a.row_lse[n] * kLog2e : 0.f;
-        weight[j] = on ? a.row_weight[n] : 0.f;
-        target[j] = on ? a.target[n] - first : -1;
-    }
-    g.template rows_out<2>(
-        [&](int i, int j, int r) __attribute__((always_inline)) {
-            const float p = fast_exp2(g.acc[i][j][r] * a.c2 - lse2[j]);
-            return weight[j] * (target[j] == i * 32 + (r / 4) * 8 + r % 4 ? p - 1.f : p);
-        },
-        [&](int n, int m, const i32x4& v) __attribute__((always_inline)) {
-            if (n0 + n < n_rows) *reinterpret_cast<i32x4*>(a.d + (size_t)(n0 + n) * a.pitch + m0 + m) = v;
-        });
+        for (int k = 0; k < 4; ++k) {
+            const float p = word + k < a.piece_n ? fast_exp2(__builtin_fmaf(l[k], a.c2, -lse2)) : 0.f;
+            d[k] = weight * (t == k ? p - 1.f : p);
+        }
+        *reinterpret_cast<bf16x4*>(a.d + (size_t)row * a.pitch + word) = pack4(d[0], d[1], d[2], d[3]);
+    });
 }
 
 // dE of the piece: D^T X, both operands with the sum's index (the row) outermost.
 template <class S>
-__global__ void __launch_bounds__(256, S::LDS_BYTES > 81920 ? 1 : 2) loss_dtable_kernel(GradArgs a) {
-    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
-    int tm, tn, unused;
-    if (!find_tile((a.hidden + S::TM - 1) / S::TM, (a.piece_n + S::TN - 1) / S::TN, 1, tm, tn, unused)) return;
-    const int n_rows = ld_const(a.count), m0 = tm * S::TM, n0 = tn * S::TN;
-    Gemm<S> g;
-    g.start(smem);
-    g.run(GemmOperand{a.rows_x + m0, a.hidden, a.hidden - m0, nullptr}, GemmOperand{a.d + n0, a.pitch, a.pitch - n0, nullptr}, n_rows);
-    const float factor = n_rows > 0 ? *a.factor : 0.f;
-    g.template rows_out<2>([&](int i, int j, int r) __attribute__((always_inline)) { return factor * g.acc[i][j][r]; },
-                           [&](int n, int m, const i32x4& v) __attribute__((always_inline)) {
-                               if (n0 + n < a.piece_n && m0 + m < a.hidden)
-                                   *reinterpret_cast<i32x4*>(a.dtable + (size_t)(a.piece0 + n0 + n) * a.hidden + m0 + m) = v;
-                           });
+__device__ __forceinline__ Work dtable_work(const GradArgs& a) {
+    return Work::make<S>(a.rows_x, a.hidden, a.hidden, a.d, a.pitch, a.piece_n, nullptr, ld_const(a.count), a.workgroups, kNever);
 }
 
-// dX: D E over the piece's words (or a split's share of them), added to what earlier pieces left.
+struct NothingAhead {
+    struct Ahead {};
+    template <class G>
+    __device__ __forceinline__ Ahead load(const G&, const GemmItem&) const { return Ahead{}; }
+};
+
 template <class S>
-__global__ void __launch_bounds__(256, S::LDS_BYTES > 81920 ? 1 : 2) loss_dx_kernel(GradArgs a) {
+struct DtableDone : NothingAhead {
+    const GradArgs& a;
+    float factor;
+    __device__ __forceinline__ DtableDone(const GradArgs& a_) : a(a_), factor(*a_.factor) {}
+    __device__ __forceinline__ void operator()(Gemm<S>& g, const GemmItem& it, Ahead, uint32_t room) const {
+        if (it.part >= 0) {
+            g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN));
+            return;
+        }
+        const int m0 = it.tm * S::TM, n0 = it.tn * S::TN;
+        g.template rows_out<2>(room, [&](int i, int j, int r) __attribute__((always_inline)) { return factor * g.sum(i, j, r); },
+                               [&](int n, int m, const i32x4& v) __attribute__((always_inline)) {
+                                   if (n0 + n < a.piece_n && m0 + m < a.hidden)
+                                       *reinterpret_cast<i32x4*>(a.dtable + (size_t)(a.piece0 + n0 + n) * a.hidden + m0 + m) = v;
+                               });
+    }
+};
+
+template <class S>
+__global__ void __launch_bounds__(256, S::PER_CU) loss_dtable_kernel(GradArgs a) {
     __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
-    const int n_rows = ld_const(a.count);
-    int tm, tn, split;
-    if (!find_tile((a.hidden + S::TM - 1) / S::TM, (n_rows + S::TN - 1) / S::TN, a.splits, tm, tn, split)) return;
-    const int steps = (a.piece_n + kStepK - 1) / kStepK, per = (steps + a.splits - 1) / a.splits;
-    const int k0 = min(split * per * kStepK, a.piece_n), k1 = min(k0 + per * kStepK, a.piece_n), m0 = tm * S::TM, n0 = tn * S::TN;
-    Gemm<S> g;
-    g.start(smem);
-    g.run(GemmOperand{a.table + (size_t)(a.piece0 + k0) * a.hidden + m0, a.hidden, a.hidden - m0, nullptr},
-          GemmOperand{a.d + (size_t)n0 * a.pitch + k0, a.pitch, n_rows - n0, nullptr}, k1 - k0);
-    const float factor = *a.factor;
-    g.template rows_out<4>([&](int i, int j, int r) __attribute__((always_inline)) { return g.acc[i][j][r]; },
-                           [&](int n, int m, const i32x4& bits) __attribute__((always_inline)) {
-                               const int row = n0 + n, col = m0 + m;
-                               if (row >= n_rows || col >= a.hidden) return;
-                               f32x4 v = __builtin_bit_cast(f32x4, bits);
-                               f32x4* part = reinterpret_cast<f32x4*>(a.part + ((size_t)split * a.n_q + row) * a.hidden + col);
-                               if (a.add) v += *part;
-                               if (a.final) *reinterpret_cast<bf16x4*>(a.dx + (size_t)a.rows[row] * a.hidden + col) = pack4(factor * v[0], factor * v[1], factor * v[2], factor * v[3]);
-                               else *part = v;
-                           });
+    const Work w = dtable_work<S>(a);
+    Gemm<S> gemm;
+    gemm.run(smem, w, DtableDone<S>(a));
 }
 
-__global__ void __launch_bounds__(256) loss_dx_join_kernel(GradArgs a) {
-    const int chunks = a.hidden / 8, strips = (chunks + 255) / 256, row = (int)blockIdx.x / strips, c = ((int)blockIdx.x % strips) * 256 + (int)threadIdx.x;
-    if (row >= *a.count || c >= chunks) return;
+template <class S>
+__global__ void __launch_bounds__(256) loss_dtable_parts_kernel(GradArgs a) {
+    const Work w = dtable_work<S>(a);
     const float factor = *a.factor;
-    f32x4 u = {0, 0, 0, 0}, v = {0, 0, 0, 0};
-    for (int s = 0; s < a.splits; ++s) {
-        const f32x4* from = reinterpret_cast<const f32x4*>(a.part + ((size_t)s * a.n_q + row) * a.hidden + c * 8);
-        u += from[0];
-        v += from[1];
+    join_parts<S>(w, a.parts, [&](int tm, int tn, int n, int m, const f32x4& v) __attribute__((always_inline)) {
+        const int word = tn * S::TN + n, col = tm * S::TM + m;
+        if (word < a.piece_n && col < a.hidden)
+            *reinterpret_cast<bf16x4*>(a.dtable + (size_t)(a.piece0 + word) * a.hidden + col) = pack4(factor * v[0], factor * v[1], factor * v[2], factor * v[3]);
+    });
+}
+
+// dX: D E over the piece's words, added to what earlier pieces left.
+template <class S>
+__device__ __forceinline__ Work dx_work(const GradArgs& a) {
+    return Work::make<S>(a.table + (size_t)a.piece0 * a.hidden, a.hidden, a.hidden, a.d, a.pitch, ld_const(a.count), nullptr, a.piece_n, a.workgroups, kNarrowParts);
+}
+
+__device__ __forceinline__ void put_dx(const GradArgs& a, float factor, int n_rows, int row, int col, f32x4 v) {
+    if (row >= n_rows || col >= a.hidden) return;
+    f32x4* sum = reinterpret_cast<f32x4*>(a.dx_sum + (size_t)row * a.hidden + col);
+    if (a.add) v += *sum;
+    if (a.final) *reinterpret_cast<bf16x4*>(a.dx + (size_t)a.rows[row] * a.hidden + col) = pack4(factor * v[0], factor * v[1], factor * v[2], factor * v[3]);
+    else *sum = v;
+}
+
+template <class S>
+struct DxDone : NothingAhead {
+    const GradArgs& a;
+    const Work& w;
+    float factor;
+    __device__ __forceinline__ DxDone(const GradArgs& a_, const Work& w_) : a(a_), w(w_), factor(*a_.factor) {}
+    __device__ __forceinline__ void operator()(Gemm<S>& g, const GemmItem& it, Ahead, uint32_t room) const {
+        if (it.part >= 0) {
+            g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN));
+            return;
+        }
+        const int m0 = it.tm * S::TM, n0 = it.tn * S::TN;
+        g.template rows_out<4>(room, [&](int i, int j, int r) __attribute__((always_inline)) { return g.sum(i, j, r); },
+                               [&](int n, int m, const i32x4& v) __attribute__((always_inline)) { put_dx(a, factor, w.qn, n0 + n, m0 + m, __builtin_bit_cast(f32x4, v)); });
     }
-    *reinterpret_cast<bf16x8*>(a.dx + (size_t)a.rows[row] * a.hidden + c * 8) =
-        pack8(factor * u[0], factor * u[1], factor * u[2], factor * u[3], factor * v[0], factor * v[1], factor * v[2], factor * v[3]);
+};
+
+template <class S>
+__global__ void __launch_bounds__(256, S::PER_CU) loss_dx_kernel(GradArgs a) {
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
+    const Work w = dx_work<S>(a);
+    Gemm<S> gemm;
+    gemm.run(smem, w, DxDone<S>(a, w));
+}
+
+template <class S>
+__global__ void __launch_bounds__(256) loss_dx_parts_kernel(GradArgs a) {
+    const Work w = dx_work<S>(a);
+    const float factor = *a.factor;
+    join_parts<S>(w, a.parts, [&](int tm, int tn, int n, int m, const f32x4& v) __attribute__((always_inline)) {
+        put_dx(a, factor, w.qn, tn * S::TN + n, tm * S::TM + m, v);
+    });
 }
 
 // ------------------------------------------------------------------------------------------
@@ -393,11 +568,16 @@ static int slot_tile(int n_q) { return n_q <= 32 ? 32 : n_q <= 64 ? 64 : n_q <= 
 constexpr size_t kPieceBytes = 512u << 20;
 constexpr int kPieceMin = 16384;
 
+static unsigned tile_grid(long long tiles) { return (unsigned)((tiles + kLists - 1) / kLists * kLists); }
+// Workgroups of a launch of wide tiles (one to a compute unit) and of a product that narrow tiles divide along k (two).
+static int wide_workgroups() { return std::max(kLists, compute_units() / kLists * kLists); }
+static int narrow_workgroups() { return 2 * wide_workgroups(); }
+
 struct LossLayout {
-    size_t off_count, off_factor, off_slot_target, off_block_count, off_block_max, off_rows, off_target, off_row_lse, off_row_weight;
+    size_t off_count, off_factor, off_slot_target, off_block_count, off_block_max, off_rows, off_target, off_row_lse, off_row_weight, off_parts;
     size_t off_part, off_target_logit, fwd_bytes;                 // forward
-    size_t off_rows_x, off_d, off_dx_part, bwd_bytes;             // backward
-    int blocks, tile, word_tiles, pitch_rows, piece, pieces, splits;
+    size_t off_rows_x, off_d, off_dx_sum, bwd_bytes;              // backward
+    int blocks, tile, word_tiles, pitch_rows, piece, pieces;
 };
 
 static LossLayout loss_layout(const wlb_vocab_desc& d) {
@@ -411,9 +591,6 @@ static LossLayout loss_layout(const wlb_vocab_desc& d) {
     size_t piece = std::max((size_t)kPieceMin, kPieceBytes / (2 * n_q) / kWordTile * kWordTile);
     L.piece = (int)std::min(words, piece);
     L.pieces = (int)((v + L.piece - 1) / L.piece);
-    const long long tiles = (long long)((d.hidden + kWordTile - 1) / kWordTile) * ((d.n_q + L.tile - 1) / L.tile);
-    const int slots = compute_units() * (L.tile <= 64 ? 2 : 1), steps = (int)((std::min((size_t)L.piece, v) + kStepK - 1) / kStepK);
-    L.splits = (int)std::max(1LL, std::min(slots / tiles, (long long)steps / 4));
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
     L.off_count = take(4);
@@ -425,6 +602,8 @@ static LossLayout loss_layout(const wlb_vocab_desc& d) {
     L.off_target = take(4 * n_q);
     L.off_row_lse = take(4 * n_q);
     L.off_row_weight = take(4 * n_q);
+    // a divided tile's parts are no more than the workgroups of the launch
+    L.off_parts = take(sizeof(float) * kWordTile * (size_t)L.tile * (L.tile < 256 ? narrow_workgroups() : wide_workgroups()));
     const size_t common = at;
     L.off_part = take(sizeof(float2) * (size_t)L.word_tiles * L.pitch_rows);
     L.off_target_logit = take(4 * n_q);
@@ -432,7 +611,7 @@ static LossLayout loss_layout(const wlb_vocab_desc& d) {
     at = common;
     L.off_rows_x = take(2 * n_q * h);
     L.off_d = take(2 * n_q * (size_t)L.piece);
-    L.off_dx_part = take(L.pieces > 1 || L.splits > 1 ? 4 * n_q * h * (size_t)L.splits : 0);
+    L.off_dx_sum = take(L.pieces > 1 ? 4 * n_q * h : 0);
     L.bwd_bytes = at;
     return L;
 }
@@ -475,6 +654,29 @@ static void launch_rows(const RowsArgs& a, hipStream_t stream) {
     }
 }
 
+// Wide tiles: one workgroup to a compute unit, and a join of the divided tiles (at most half as many as there are workgroups) where `depth` is long enough.
+template <class K, class J, class A>
+static void launch_wide(K kernel, J join, A& a, int depth, hipStream_t stream) {
+    a.workgroups = wide_workgroups();
+    kernel<<<a.workgroups, 256, 0, stream>>>(a);
+    if ((depth + kStepK - 1) / kStepK >= 2 * kWideParts) join<<<a.workgroups / 2 * 256 / 4, 256, 0, stream>>>(a);
+}
+
+// Narrow tiles, one to a workgroup.
+template <class K, class A>
+static void launch_narrow(K kernel, A& a, long long tiles, hipStream_t stream) {
+    a.workgroups = (int)tile_grid(tiles);
+    kernel<<<a.workgroups, 256, 0, stream>>>(a);
+}
+
+// Narrow tiles along the columns, all divided along the words.  tile: slots of one
+template <class K, class J, class A>
+static void launch_divided(K kernel, J join, A& a, int tile, int tiles, hipStream_t stream) {
+    a.workgroups = narrow_workgroups();
+    kernel<<<a.workgroups, 256, 0, stream>>>(a);
+    join<<<std::min(tiles, a.workgroups / 2) * tile / 4, 256, 0, stream>>>(a);
+}
+
 }  // namespace wlb
 
 using namespace wlb;
@@ -507,12 +709,12 @@ extern "C" wlb_status wlb_loss_fwd(const wlb_vocab_desc* desc, const void* x, co
     a.rows = r.rows; a.target = r.target; a.count = r.count;
     a.part = (float2*)(ws + L.off_part); a.target_logit = (float*)(ws + L.off_target_logit);
     a.vocab = d.vocab; a.hidden = d.hidden; a.pitch = L.pitch_rows; a.c2 = d.scale * kLog2e;
-    const unsigned grid = tile_grid((long long)L.word_tiles * ((d.n_q + L.tile - 1) / L.tile));
-    if (L.tile == 32) loss_stats_kernel<Slots32<false, false>><<<grid, 256, 0, stream>>>(a);
-    else if (L.tile == 64) loss_stats_kernel<Slots64<false, false>><<<grid, 256, 0, stream>>>(a);
-    else if (L.tile == 128) loss_stats_kernel<Slots128<false, false>><<<grid, 256, 0, stream>>>(a);
-    else loss_stats_kernel<Wide<false, false>><<<grid, 256, 0, stream>>>(a);
-    loss_join_kernel<<<(d.n_q + 31) / 32, 256, 0, stream>>>(a.part, a.target_logit, a.rows, a.count, loss, lse, L.word_tiles, L.pitch_rows, d.scale);
+    a.parts = (float*)(ws + L.off_parts);
+    if (L.tile == 32) launch_narrow(loss_stats_kernel<Slots32<false, false>>, a, L.word_tiles, stream);
+    else if (L.tile == 64) launch_narrow(loss_stats_kernel<Slots64<false, false>>, a, L.word_tiles, stream);
+    else if (L.tile == 128) launch_narrow(loss_stats_kernel<Slots128<false, false>>, a, L.word_tiles, stream);
+    else launch_wide(loss_stats_kernel<Wide<false, false>>, loss_stats_parts_kernel<Wide<false, false>>, a, d.hidden, stream);
+    loss_join_kernel<<<(d.n_q + 31) / 32, 256, 0, stream>>>(a.part, a.target_logit, a.rows, a.count, loss, lse, L.word_tiles, L.pitch_rows, a.c2);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(WLB_ERR_HIP, "loss launch: %s", hipGetErrorString(e));
     return WLB_OK;
@@ -537,31 +739,30 @@ extern "C" wlb_status wlb_loss_bwd(const wlb_vocab_desc* desc, const void* x, co
     launch_rows(r, stream);
     GradArgs a = {};
     a.table = (const __bf16*)table; a.rows_x = (__bf16*)(ws + L.off_rows_x); a.d = (__bf16*)(ws + L.off_d);
-    a.dx = (__bf16*)dx; a.dtable = (__bf16*)dtable; a.part = (float*)(ws + L.off_dx_part);
+    a.dx = (__bf16*)dx; a.dtable = (__bf16*)dtable; a.dx_sum = (float*)(ws + L.off_dx_sum);
     a.rows = r.rows; a.target = r.target; a.count = r.count; a.row_lse = r.row_lse; a.row_weight = r.row_weight; a.factor = r.factor;
-    a.vocab = d.vocab; a.hidden = d.hidden; a.n_q = d.n_q; a.pitch = L.piece; a.splits = L.splits; a.c2 = d.scale * kLog2e;
+    a.vocab = d.vocab; a.hidden = d.hidden; a.n_q = d.n_q; a.pitch = L.piece; a.c2 = d.scale * kLog2e;
     loss_gather_kernel<<<(d.n_q + 3) / 4, 256, 0, stream>>>((const uint4*)x, (uint4*)a.rows_x, (uint4*)dx, a.rows, r.slot_target, a.count, d.n_q, d.hidden / 8);
-    const long long slot_tiles = (d.n_q + L.tile - 1) / L.tile;
+    a.parts = (float*)(ws + L.off_parts);
     for (int p = 0; p < L.pieces; ++p) {
         a.piece0 = p * L.piece;
         a.piece_n = std::min(L.piece, d.vocab - a.piece0);
         a.add = p > 0;
-        a.final = p == L.pieces - 1 && L.splits == 1;
-        const unsigned d_grid = tile_grid((long long)((a.piece_n + kWordTile - 1) / kWordTile) * slot_tiles);
-        if (L.tile == 32) loss_d_kernel<Slots32<false, false>><<<d_grid, 256, 0, stream>>>(a);
-        else if (L.tile == 64) loss_d_kernel<Slots64<false, false>><<<d_grid, 256, 0, stream>>>(a);
-        else if (L.tile == 128) loss_d_kernel<Slots128<false, false>><<<d_grid, 256, 0, stream>>>(a);
-        else loss_d_kernel<Wide<false, false>><<<d_grid, 256, 0, stream>>>(a);
-        const long long wide = (long long)((a.piece_n + 255) / 256) * ((d.hidden + 255) / 256);
-        if (wide >= compute_units()) loss_dtable_kernel<Wide<true, true>><<<tile_grid(wide), 256, 0, stream>>>(a);
-        else loss_dtable_kernel<Half<true, true>><<<tile_grid((long long)((a.piece_n + 127) / 128) * ((d.hidden + 127) / 128)), 256, 0, stream>>>(a);
-        const unsigned dx_grid = tile_grid((long long)((d.hidden + kWordTile - 1) / kWordTile) * slot_tiles * L.splits);
-        if (L.tile == 32) loss_dx_kernel<Slots32<true, false>><<<dx_grid, 256, 0, stream>>>(a);
-        else if (L.tile == 64) loss_dx_kernel<Slots64<true, false>><<<dx_grid, 256, 0, stream>>>(a);
-        else if (L.tile == 128) loss_dx_kernel<Slots128<true, false>><<<dx_grid, 256, 0, stream>>>(a);
-        else loss_dx_kernel<Wide<true, false>><<<dx_grid, 256, 0, stream>>>(a);
+        a.final = p == L.pieces - 1;
+        const int word_tiles = (a.piece_n + kWordTile - 1) / kWordTile, column_tiles = (d.hidden + kWordTile - 1) / kWordTile;
+        if (L.tile == 32) launch_narrow(loss_d_kernel<Slots32<false, false>>, a, word_tiles, stream);
+        else if (L.tile == 64) launch_narrow(loss_d_kernel<Slots64<false, false>>, a, word_tiles, stream);
+        else if (L.tile == 128) launch_narrow(loss_d_kernel<Slots128<false, false>>, a, word_tiles, stream);
+        else launch_wide(loss_d_kernel<Wide<false, false>>, loss_d_parts_kernel<Wide<false, false>>, a, d.hidden, stream);
+        // tiles of 128 x 128 where wide ones neither fill the launch nor have rows enough to be divided
+        if ((long long)word_tiles * column_tiles >= wide_workgroups() || d.n_q >= 2 * kWideParts * kStepK)
+            launch_wide(loss_dtable_kernel<Wide<true, true>>, loss_dtable_parts_kernel<Wide<true, true>>, a, d.n_q, stream);
+        else launch_narrow(loss_dtable_kernel<Half<true, true>>, a, (long long)((a.piece_n + 127) / 128) * ((d.hidden + 127) / 128), stream);
+        if (L.tile == 32) launch_divided(loss_dx_kernel<Slots32<true, false>>, loss_dx_parts_kernel<Slots32<true, false>>, a, 32, column_tiles, stream);
+        else if (L.tile == 64) launch_divided(loss_dx_kernel<Slots64<true, false>>, loss_dx_parts_kernel<Slots64<true, false>>, a, 64, column_tiles, stream);
+        else if (L.tile == 128) launch_divided(loss_dx_kernel<Slots128<true, false>>, loss_dx_parts_kernel<Slots128<true, false>>, a, 128, column_tiles, stream);
+        else launch_wide(loss_dx_kernel<Wide<true, false>>, loss_dx_parts_kernel<Wide<true, false>>, a, a.piece_n, stream);
     }
-    if (L.splits > 1) loss_dx_join_kernel<<<(unsigned)d.n_q * ((d.hidden / 8 + 255) / 256), 256, 0, stream>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(WLB_ERR_HIP, "loss gradient launch: %s", hipGetErrorString(e));
     return WLB_OK;
