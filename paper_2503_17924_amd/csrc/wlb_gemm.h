@@ -1,10 +1,11 @@
 // Matrix products of the loss over the vocabulary: D[m][n] = sum_k P[m][k] * Q[n][k], bf16 operands, fp32 sums.
 //
-// Four wavefronts, each WM-th x WN-th part of a tile of TM x TN.  Operands move global -> LDS by buffer_load ... lds in
-// steps of 64 along k, and LDS -> registers one 16-step ahead of the MFMAs.  An operand lies in memory either with k
+// Four wavefronts, each WM-th x WN-th part of a tile of TM x TN, in blocks of 16 x 16 x 32 (the power limit lets 16x16x32 MFMAs run at 1.73 - 1.80
+// PFLOP/s on random operands and 32x32x16 ones at 1.64 - 1.68).  Operands move global -> LDS by buffer_load ... lds in
+// steps of 64 along k, and LDS -> registers one 32-step ahead of the MFMAs.  An operand lies in memory either with k
 // contiguous (rows of m or n: "K") or with m or n contiguous (rows of k: "M"); the second kind is read from LDS with transpose reads, so
 // no operand is ever written transposed.  Wide tiles (256 x 256) take one workgroup to a compute unit and one wavefront to a SIMD: a wavefront's
-// 128 x 128 part needs 8 KiB of LDS reads for 16 MFMAs, half of what 8 wavefronts of 128 x 64 would read.  They are bound by the MFMA rate at
+// 128 x 128 part needs 16 KiB of LDS reads for 64 MFMAs, two thirds of what 8 wavefronts of 128 x 64 would read.  They are bound by the MFMA rate at
 // the clock that the power limit leaves (1.5 - 1.8 GHz).  Narrow tiles (few slots) are bound by the table's bytes.
 #pragma once
 #include <type_traits>
@@ -14,14 +15,22 @@
 namespace wlb {
 
 constexpr int kStepK = 64;
+
+// D[16x16] += A[16x32] * B[32x16], one wavefront.  Lane l supplies A[l%16][8*(l/16) .. +7] and B[8*(l/16) .. +7][l%16];
+// accumulator register r of lane l is D[(l/16)*4 + r][l%16].
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// Place of 16-byte chunk cc of row r in an LDS tile of kind M: a transpose read takes 8 rows (r % 4, and 8 apart) x 2 chunks at a time, which
+// this puts on 16 different chunks of 256 bytes.
+__device__ __forceinline__ int swz_m(int r, int cc) { return cc ^ (((r & 3) << 2) | (((r >> 3) & 1) << 1)); }
 constexpr int kOutOfRange = (int)0xfffffff0u;      // a lane offset at which every buffer load returns 0
 constexpr uint32_t kMaxRecords = 0xffffffe0u;
 
 template <int WM_, int WN_, int BM_, int BN_, bool MP_, bool MQ_>
 struct GemmShape {
-    static constexpr int WM = WM_, WN = WN_, BM = BM_, BN = BN_;         // wavefronts, and blocks of 32 of a wavefront
+    static constexpr int WM = WM_, WN = WN_, BM = BM_, BN = BN_;         // wavefronts, and blocks of 16 of a wavefront
     static constexpr bool MP = MP_, MQ = MQ_;                            // operand kinds: m / n contiguous in memory
-    static constexpr int TM = WM * BM * 32, TN = WN * BN * 32;
+    static constexpr int TM = WM * BM * 16, TN = WN * BN * 16;
     static constexpr int P_BYTES = TM * kStepK * 2, Q_BYTES = TN * kStepK * 2, STAGE = P_BYTES + Q_BYTES;
     // Five LDS slots of one operand's tile, or two buffers of both tiles
     static constexpr bool RING = P_BYTES == 32768 && Q_BYTES == 32768;
@@ -107,7 +116,7 @@ struct TileCopy {
     int wave, lane, left;                                       // k that exist from this step's start on
 
     __device__ __forceinline__ int row_of(int n) const { return (wave * N + n) * RPI + lane / CH; }
-    __device__ __forceinline__ int chunk_of(int n) const { return M ? (lane % CH) ^ ((row_of(n) & 3) << 2) : swz<8>(row_of(n), lane % 8); }
+    __device__ __forceinline__ int chunk_of(int n) const { return M ? swz_m(row_of(n), lane % CH) : swz<8>(row_of(n), lane % 8); }
     // ld: elements between rows
     __device__ __forceinline__ void init(long long ld, int wave_, int lane_) {
         row_bytes = (uint32_t)(ld * 2);
@@ -149,38 +158,38 @@ struct TileCopy {
     __device__ __forceinline__ void issue(int n, uint32_t lds_tile) const { dma_issue_1k(rs.r, lds_tile + (uint32_t)(wave * N + n) * 1024u, voff[n], 0u); }
 };
 
-// Operand fragments of a wavefront out of LDS: B blocks of 32 rows (columns).
+// Operand fragments of a wavefront out of LDS: B blocks of 16 rows (columns).
 template <int T, int B, bool M>
 struct Fragments {
     static constexpr int READS = M ? 2 * B : B;
-    uint32_t at[M ? B : 4];         // K: by 16-step, the blocks 4096 bytes apart; M: by block, the 16-steps 16 rows apart
+    uint32_t at[M ? B : 2];         // K: by 32-step, the blocks 2048 bytes apart; M: by block, the 32-steps 32 rows apart
 
     __device__ __forceinline__ void init(uint32_t tile, int first, int lane) {
         if (M) {
 #pragma unroll
             for (int i = 0; i < B; ++i) {
-                const int row = 8 * (lane / 32) + (lane % 16) / 4, chunk = (first + i) * 4 + 2 * ((lane / 16) & 1) + (lane % 4) / 2;
-                at[i] = tile + row * (T * 2) + (chunk ^ ((row & 3) << 2)) * 16 + (lane % 2) * 8;
+                const int row = 8 * (lane / 16) + (lane % 16) / 4, chunk = (first + i) * 2 + (lane % 4) / 2;
+                at[i] = tile + row * (T * 2) + swz_m(row, chunk) * 16 + (lane % 2) * 8;
             }
         } else {
-            const int row = first * 32 + lane % 32;
+            const int row = first * 16 + lane % 16;
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) at[kk] = tile + row * 128 + swz<8>(row, 2 * kk + lane / 32) * 16;
+            for (int kk = 0; kk < 2; ++kk) at[kk] = tile + row * 128 + swz<8>(row, 4 * kk + lane / 16) * 16;
         }
     }
     __device__ __forceinline__ void move(int bytes) {
 #pragma unroll
-        for (int i = 0; i < (M ? B : 4); ++i) at[i] += bytes;
+        for (int i = 0; i < (M ? B : 2); ++i) at[i] += bytes;
     }
-    // read r of READS of 16-step kk into f
+    // read r of READS of 32-step kk into f
     __device__ __forceinline__ void read(int r, int kk, bf16x8 (&f)[B]) const {
         if (M) {
             const int i = r / 2, h = r % 2;
-            const bf16x4 v = lds_read_tr4_at(at[i] + kk * 16 * T * 2 + h * 4 * T * 2);
+            const bf16x4 v = lds_read_tr4_at(at[i] + kk * 32 * T * 2 + h * 4 * T * 2);
 #pragma unroll
             for (int e = 0; e < 4; ++e) f[i][4 * h + e] = v[e];
         } else {
-            f[r] = *reinterpret_cast<const WLB_LDS bf16x8*>((uintptr_t)(at[kk] + r * 4096));
+            f[r] = *reinterpret_cast<const WLB_LDS bf16x8*>((uintptr_t)(at[kk] + r * 2048));
         }
     }
 };
@@ -189,7 +198,7 @@ struct Fragments {
 // item; lds: 32 KiB, 8 of them each wavefront's own; ahead: what done.load(gemm, item) returned in front of the item's steps (loads that would hold up its end).
 template <class S>
 struct Gemm {
-    f32x16 acc[S::BM][S::BN];   // register r of lane l: m = 32 i + (r/4)*8 + (l/32)*4 + r%4, n = 32 j + l%32 of the wavefront's part
+    f32x4 acc[S::BM][S::BN];    // register r of lane l: m = 16 i + (l/16)*4 + r, n = 16 j + l%16 of the wavefront's part
     int wave, lane, wm, wn;
     uint32_t lds;
     TileCopy<S::TM, S::MP> cp;
@@ -206,7 +215,7 @@ struct Gemm {
 #pragma unroll
             for (int j = 0; j < S::BN; ++j)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+                for (int r = 0; r < 4; ++r) acc[i][j][r] = 0.f;
     }
 
     template <class Work, class Done>
@@ -256,8 +265,8 @@ struct Gemm {
             for (int s = 0; s < steps; ++s) {
                 const uint32_t stage = lds + (s & 1) * S::STAGE;
 #pragma unroll
-                for (int kk = 0; kk < 4; ++kk) {
-                    if (kk == 3) {
+                for (int kk = 0; kk < 2; ++kk) {
+                    if (kk == 1) {
                         // the step's last operands are in registers and the next step's tiles in LDS, for every wavefront
                         wait_lds();
                         wait_vmem();
@@ -271,17 +280,17 @@ struct Gemm {
                         fq.move(flip);
                     }
 #pragma unroll
-                    for (int x = 0; x < BM * BN || x < RP + RQ || (kk == 3 && x < NP + NQ); ++x) {
-                        // reads of the operands of the next 16-step, copies of the step after the next, MFMAs of this one
-                        if (x < RQ) fq.read(x, (kk + 1) & 3, b[(kk + 1) & 1]);
-                        else if (x < RP + RQ) fp.read(x - RQ, (kk + 1) & 3, a[(kk + 1) & 1]);
-                        if (kk == 3) {
+                    for (int x = 0; x < BM * BN || x < RP + RQ || (kk == 1 && x < NP + NQ); ++x) {
+                        // reads of the operands of the next 32-step, copies of the step after the next, MFMAs of this one
+                        if (x < RQ) fq.read(x, kk ^ 1, b[kk ^ 1]);
+                        else if (x < RP + RQ) fp.read(x - RQ, kk ^ 1, a[kk ^ 1]);
+                        if (kk == 1) {
                             if (x < NP) cp.issue(x, stage);
                             else if (x < NP + NQ) cq.issue(x - NP, stage + S::P_BYTES);
                         }
                         if (x < BM * BN) {
                             const int i = x / BN, j = x % BN;
-                            acc[i][j] = mfma32(a[kk & 1][i], b[kk & 1][j], acc[i][j]);
+                            acc[i][j] = mfma16(a[kk][i], b[kk][j], acc[i][j]);
                         }
                         __builtin_amdgcn_sched_barrier(0);
                     }
@@ -299,13 +308,13 @@ struct Gemm {
     // Wide tiles.  The operands' tiles P0 Q0 P1 Q1 .. go to five LDS slots in turn, and on without a break from one item to the next:
     // while an item's sums go to memory, the first two steps of the next are in LDS or on their way, and the slot that is left holds the output.  Copies
     // take half of the time that the vector memory path has (64 KiB of 128 a step), so they are spread over the step: four wavefronts that
-    // issued all of them in one quarter of it waited for each other (72 % of the time).  Step s copies P of s + 2 beside its first three
-    // 16-steps, into the slot that Q of s - 1 left, and behind the step's barrier Q of s + 2 into the slot of its own P.  An item has two steps
+    // issued all of them in one quarter of it waited for each other (10 % more time).  Step s copies P of s + 2 beside its first
+    // 32-step, into the slot that Q of s - 1 left, and behind the step's barrier Q of s + 2 into the slot of its own P.  An item has two steps
     // at least (the second may be zeros), so that the steps two ahead of its last two are the next item's first two.
     template <class Work, class Done>
     __device__ __forceinline__ void ring(const Work& work, const Done& done) {
         constexpr int BM = S::BM, BN = S::BN, SLOT = S::P_BYTES;
-        static_assert(NP == 8 && NQ == 8 && BM * BN == 16 && RP + RQ <= 16, "where in a step the copies stand");
+        static_assert(NP == 8 && NQ == 8 && BM * BN == 64 && RP + RQ <= 32, "where in a step the copies stand");
         GemmItem it, next;
         if (!work.item((int)blockIdx.x, 0, it)) return;
         cp.tile(work.p(it));
@@ -331,9 +340,7 @@ struct Gemm {
         for (int r = 0; r < RP; ++r) fp.read(r, 0, a[0]);
 #pragma unroll
         for (int r = 0; r < RQ; ++r) fq.read(r, 0, b[0]);
-        f32x16 zeros;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) zeros[r] = 0.f;
+        const f32x4 zeros = {0.f, 0.f, 0.f, 0.f};
         int p_slot = 0, q_slot = 1;             // of this step's tiles
         for (int round = 1;; ++round) {
             const int steps = steps_of(it, 2);
@@ -351,8 +358,8 @@ struct Gemm {
                 cp.cut();
                 const uint32_t to_p = lds + (p_slot == 0 ? 4 : p_slot - 1) * SLOT, to_q = lds + p_slot * SLOT;
 #pragma unroll
-                for (int kk = 0; kk < 4; ++kk) {
-                    if (kk == 3) {
+                for (int kk = 0; kk < 2; ++kk) {
+                    if (kk == 1) {
                         // the step's last operands are in registers and the next step's tiles in LDS, for every wavefront
                         wait_lds();
                         wait_vmem_le<NP>();
@@ -371,15 +378,17 @@ struct Gemm {
                         q_slot += q_move;
                     }
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        // reads of the operands of the next 16-step, copies, MFMAs of this one
-                        if (x < RQ) fq.read(x, (kk + 1) & 3, b[(kk + 1) & 1]);
-                        else if (x < RP + RQ) fp.read(x - RQ, (kk + 1) & 3, a[(kk + 1) & 1]);
-                        if (kk == 3 && x % 2 == 1) cq.issue(x / 2, to_q);
-                        if (kk < 3 && (kk * 16 + x) % 6 == 2) cp.issue((kk * 16 + x) / 6, to_p);
+                    for (int x = 0; x < 64; ++x) {
+                        // reads of the operands of the next 32-step, copies, MFMAs of this one
+                        if (x % 2 == 0) {
+                            if (x / 2 < RQ) fq.read(x / 2, kk ^ 1, b[kk ^ 1]);
+                            else if (x / 2 < RP + RQ) fp.read(x / 2 - RQ, kk ^ 1, a[kk ^ 1]);
+                        }
+                        if (kk == 1 && x % 5 == 1 && x < 40) cq.issue(x / 5, to_q);
+                        if (kk == 0 && x % 8 == 3) cp.issue(x / 8, to_p);
                         const int i = x / BN, j = x % BN;
-                        acc[i][j] = mfma32(a[kk & 1][i], b[kk & 1][j], fresh && kk == 0 ? zeros : acc[i][j]);
-                        __builtin_amdgcn_sched_barrier(0);
+                        acc[i][j] = mfma16(a[kk][i], b[kk][j], fresh && kk == 0 ? zeros : acc[i][j]);
+                        if (x % 2 == 1) __builtin_amdgcn_sched_barrier(0);
                     }
                 }
             };
@@ -406,41 +415,40 @@ struct Gemm {
     __device__ __forceinline__ void sums_ready() const {
         if constexpr (!S::RING) return;
         __builtin_amdgcn_sched_barrier(0);
-        asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");       // an MFMA's result: 19 wait states
+        asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");       // an MFMA's result: 11 wait states, 19 for one of 16 passes
         __builtin_amdgcn_sched_barrier(0);
     }
 
-    // Rows of output through LDS, so that memory sees whole 256-byte pieces: `Bytes` = 2 (bf16: all of the wavefront's 32 BM values of a row)
-    // or 4 (fp32: two blocks at a time).  value(i, j, r) gives the values; put(n, m, bits) takes 16 bytes: n, m counted in the tile.
+    // Rows of output through LDS, so that memory sees whole 256-byte pieces: 32 rows n at a time (16 where there are no more), `Bytes` = 2 (bf16: all of the
+    // wavefront's values of a row) or 4 (fp32: up to 64 of them).  value(i, j, r) gives the values; put(n, m, bits) takes 16 bytes: n, m counted in the tile.
     template <int Bytes, class V, class Put>
     __device__ __forceinline__ void rows_out(uint32_t room, V value, Put put) {
-        constexpr int G = Bytes == 2 ? (S::BM < 4 ? S::BM : 4) : (S::BM < 2 ? S::BM : 2);        // blocks of 32 m at a time
-        constexpr int ROWB = G * 32 * Bytes, CH = ROWB / 16, RPI = 64 / CH;                      // bytes, chunks of a row; rows per pass
-        static_assert(S::BM % G == 0 && ROWB <= 256, "8 KiB of a wavefront");
+        constexpr int MOST = 256 / (16 * Bytes), G = S::BM < MOST ? S::BM : MOST, H = S::BN < 2 ? S::BN : 2;    // blocks of 16 m, of 16 n at a time
+        constexpr int ROWB = G * 16 * Bytes, CH = ROWB / 16, RPI = 64 / CH;                      // bytes, chunks of a row; rows per pass
+        static_assert(S::BM % G == 0 && S::BN % H == 0 && ROWB <= 256 && 16 * H % RPI == 0, "8 KiB of a wavefront");
         const uint32_t mine = room + wave * 8192;
 #pragma unroll
-        for (int j = 0; j < S::BN; ++j)
+        for (int j0 = 0; j0 < S::BN; j0 += H)
 #pragma unroll
             for (int i0 = 0; i0 < S::BM; i0 += G) {
-                const int row = lane % 32;
 #pragma unroll
-                for (int i = 0; i < G; ++i)
+                for (int j = 0; j < H; ++j)
 #pragma unroll
-                    for (int r = 0; r < 16; r += 4) {
-                        const int m = i * 32 + (r / 4) * 8 + (lane / 32) * 4, byte = m * Bytes;
+                    for (int i = 0; i < G; ++i) {
+                        const int row = j * 16 + lane % 16, byte = (i * 16 + (lane / 16) * 4) * Bytes;
                         const uint32_t to = mine + row * ROWB + (((byte / 16) ^ (row & (CH - 1))) * 16) + byte % 16;
-                        const float v0 = value(i0 + i, j, r), v1 = value(i0 + i, j, r + 1), v2 = value(i0 + i, j, r + 2), v3 = value(i0 + i, j, r + 3);
+                        const float v0 = value(i0 + i, j0 + j, 0), v1 = value(i0 + i, j0 + j, 1), v2 = value(i0 + i, j0 + j, 2), v3 = value(i0 + i, j0 + j, 3);
                         if (Bytes == 2) *reinterpret_cast<WLB_LDS bf16x4*>((uintptr_t)to) = pack4(v0, v1, v2, v3);
                         else *reinterpret_cast<WLB_LDS f32x4*>((uintptr_t)to) = f32x4{v0, v1, v2, v3};
-                        if (r == 12) __builtin_amdgcn_sched_barrier(0);         // few values out of the accumulators at a time
+                        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);      // few values out of the accumulators at a time
                     }
                 wait_lds();
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                for (int t = 0; t < 32 / RPI; ++t) {
+                for (int t = 0; t < 16 * H / RPI; ++t) {
                     const int n = t * RPI + lane / CH, c = lane % CH;
                     const i32x4 v = *reinterpret_cast<const WLB_LDS i32x4*>((uintptr_t)(mine + n * ROWB + ((c ^ (n & (CH - 1))) * 16)));
-                    put(wn * (S::BN * 32) + j * 32 + n, wm * (S::BM * 32) + i0 * 32 + c * 16 / Bytes, v);
+                    put(wn * (S::BN * 16) + j0 * 16 + n, wm * (S::BM * 16) + i0 * 16 + c * 16 / Bytes, v);
                 }
                 wait_lds();
                 __builtin_amdgcn_wave_barrier();

@@ -204,18 +204,25 @@ __device__ __forceinline__ Work stats_work(const StatsArgs& a) {
     return Work::make<S>(a.table, a.hidden, a.vocab, a.x, a.hidden, n_rows, a.rows, a.hidden, a.workgroups, kNever);
 }
 
+// What belongs to a wavefront's rows n is loaded once for every row, 64 to a register, and fetched from the lane that holds it.
+template <class S> constexpr int row_regs() { return (S::BN * 16 + 63) / 64; }
+template <class S>
+__device__ __forceinline__ int row_held(const Gemm<S>& g, const GemmItem& it, int k) { return it.tn * S::TN + g.wn * (S::BN * 16) + k * 64 + g.lane % (S::BN * 16); }
+template <class T, int N>
+__device__ __forceinline__ T of_row(const T (&regs)[N], int j, int lane) { return __shfl(regs[j / 4], (j % 4) * 16 + lane % 16); }
+
 template <class S>
 struct StatsDone {
     const StatsArgs& a;
     const Work& w;
     char* smem;
-    struct Ahead { int target[S::BN]; };        // of the lane's rows, -1: no row
+    struct Ahead { int target[row_regs<S>()]; };        // -1: no row
     __device__ __forceinline__ Ahead load(const Gemm<S>& g, const GemmItem& it) const {
         Ahead h;
 #pragma unroll
-        for (int j = 0; j < S::BN; ++j) {
-            const int row = it.tn * S::TN + g.wn * (S::BN * 32) + j * 32 + g.lane % 32;
-            h.target[j] = row < w.qn ? a.target[row] : -1;
+        for (int k = 0; k < row_regs<S>(); ++k) {
+            const int row = row_held<S>(g, it, k);
+            h.target[k] = row < w.qn ? a.target[row] : -1;
         }
         return h;
     }
@@ -225,38 +232,40 @@ struct StatsDone {
             return;
         }
         const int m0 = it.tm * S::TM, n0 = it.tn * S::TN, n_rows = w.qn;
-        const int first = m0 + g.wm * (S::BM * 32) + (g.lane / 32) * 4;       // word of register 0 of block 0
+        const int first = m0 + g.wm * (S::BM * 16) + (g.lane / 16) * 4;       // word of register 0 of block 0
         float2* s_part = (float2*)(smem + (room - g.lds));                    // [WM][TN]
         auto block = [&](int j, auto edge) __attribute__((always_inline)) {   // edge: words of the tile lie past the end
-            const int n = g.wn * (S::BN * 32) + j * 32 + g.lane % 32;
+            const int n = g.wn * (S::BN * 16) + j * 16 + g.lane % 16;
             auto logit = [&](int i, int r) __attribute__((always_inline)) {
                 const float l = g.sum(i, j, r);
-                return edge && first + i * 32 + (r / 4) * 8 + r % 4 >= a.vocab ? -INFINITY : l;
+                return edge && first + i * 16 + r >= a.vocab ? -INFINITY : l;
             };
-            const int t = ahead.target[j] < 0 ? -1 : ahead.target[j] - first;    // register that holds the target, if this lane has it
+            const int word = of_row(ahead.target, j, g.lane), t = word < 0 ? -1 : word - first;    // register that holds the target, if this lane has it
             float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
             for (int i = 0; i < S::BM; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) most[r % 4] = fmaxf(most[r % 4], logit(i, r));
+                for (int r = 0; r < 4; ++r) most[r] = fmaxf(most[r], logit(i, r));
             float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+            top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, xhalf(top));
-            if (__any(t >= 0 && t < S::BM * 32)) {
+            if (__any(t >= 0 && t < S::BM * 16)) {
 #pragma unroll
                 for (int i = 0; i < S::BM; ++i)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (t == i * 32 + (r / 4) * 8 + r % 4) a.target_logit[n0 + n] = g.sum(i, j, r);
+                    for (int r = 0; r < 4; ++r)
+                        if (t == i * 16 + r) a.target_logit[n0 + n] = g.sum(i, j, r);
             }
             const float ref = top == -INFINITY ? -INFINITY : top * a.c2, from = top == -INFINITY ? 0.f : ref;    // a wavefront all of whose words lie past the end
             float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < S::BM; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) sum[r % 4] += fast_exp2(__builtin_fmaf(logit(i, r), a.c2, -from));
+                for (int r = 0; r < 4; ++r) sum[r] += fast_exp2(__builtin_fmaf(logit(i, r), a.c2, -from));
             float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            all += __shfl_xor(all, 16);
             all += xhalf(all);
-            if (g.lane < 32) s_part[g.wm * S::TN + n] = float2{ref, all};
+            if (g.lane < 16) s_part[g.wm * S::TN + n] = float2{ref, all};
             __builtin_amdgcn_sched_barrier(0);
         };
         if (m0 + S::TM > a.vocab) {
@@ -392,16 +401,16 @@ template <class S>
 struct DDone {
     const GradArgs& a;
     const Work& w;
-    struct Ahead { float lse[S::BN], weight[S::BN]; int target[S::BN]; };       // of the lane's rows
+    struct Ahead { float lse2[row_regs<S>()], weight[row_regs<S>()]; int target[row_regs<S>()]; };
     __device__ __forceinline__ Ahead load(const Gemm<S>& g, const GemmItem& it) const {
         Ahead h;
 #pragma unroll
-        for (int j = 0; j < S::BN; ++j) {
-            const int row = it.tn * S::TN + g.wn * (S::BN * 32) + j * 32 + g.lane % 32;
+        for (int k = 0; k < row_regs<S>(); ++k) {
+            const int row = row_held<S>(g, it, k);
             const bool on = row < w.qn;
-            h.lse[j] = on ? a.row_lse[row] : 0.f;
-            h.weight[j] = on ? a.row_weight[row] : 0.f;
-            h.target[j] = on ? a.target[row] : -1;
+            h.lse2[k] = on ? a.row_lse[row] : 0.f;
+            h.weight[k] = on ? a.row_weight[row] : 0.f;
+            h.target[k] = on ? a.target[row] : -1;
         }
         return h;
     }
@@ -411,14 +420,22 @@ struct DDone {
             return;
         }
         const int m0 = it.tm * S::TM, n0 = it.tn * S::TN;
-        const int first = m0 + g.wm * (S::BM * 32) + (g.lane / 32) * 4;     // word of register 0 of block 0, in the piece
+        const int first = m0 + g.wm * (S::BM * 16) + (g.lane / 16) * 4;     // word of register 0 of block 0, in the piece
+        float lse2[S::BN], weight[S::BN];
+        int target[S::BN];
+#pragma unroll
+        for (int j = 0; j < S::BN; ++j) {
+            lse2[j] = of_row(h.lse2, j, g.lane) * kLog2e;
+            weight[j] = of_row(h.weight, j, g.lane);
+            target[j] = of_row(h.target, j, g.lane) - a.piece0 - first;
+        }
         auto out = [&](auto edge) __attribute__((always_inline)) {          // edge: words of the tile lie past the end, D is 0 there
             g.template rows_out<2>(
                 room,
                 [&](int i, int j, int r) __attribute__((always_inline)) {
-                    const int word = i * 32 + (r / 4) * 8 + r % 4;
-                    const float e = fast_exp2(__builtin_fmaf(g.sum(i, j, r), a.c2, -h.lse[j] * kLog2e)), p = edge && first + word >= a.piece_n ? 0.f : e;
-                    return h.weight[j] * (h.target[j] - a.piece0 - first == word ? p - 1.f : p);
+                    const int word = i * 16 + r;
+                    const float e = fast_exp2(__builtin_fmaf(g.sum(i, j, r), a.c2, -lse2[j])), p = edge && first + word >= a.piece_n ? 0.f : e;
+                    return weight[j] * (target[j] == word ? p - 1.f : p);
                 },
                 [&](int n, int m, const i32x4& v) __attribute__((always_inline)) {
                     if (n0 + n < w.qn) *reinterpret_cast<i32x4*>(a.d + (size_t)(n0 + n) * a.pitch + m0 + m) = v;
@@ -555,11 +572,11 @@ __global__ void __launch_bounds__(256) loss_dx_parts_kernel(GradArgs a) {
 
 // ------------------------------------------------------------------------------------------
 // Tiles.  `Slots32` .. `Slots128` serve calls of few slots: four wavefronts side by side along the words (or columns).
-template <bool MP, bool MQ> using Wide = GemmShape<2, 2, 4, 4, MP, MQ>;
-template <bool MP, bool MQ> using Half = GemmShape<2, 2, 2, 2, MP, MQ>;
-template <bool MP, bool MQ> using Slots128 = GemmShape<4, 1, 2, 4, MP, MQ>;
-template <bool MP, bool MQ> using Slots64 = GemmShape<4, 1, 2, 2, MP, MQ>;
-template <bool MP, bool MQ> using Slots32 = GemmShape<4, 1, 2, 1, MP, MQ>;
+template <bool MP, bool MQ> using Wide = GemmShape<2, 2, 8, 8, MP, MQ>;
+template <bool MP, bool MQ> using Half = GemmShape<2, 2, 4, 4, MP, MQ>;
+template <bool MP, bool MQ> using Slots128 = GemmShape<4, 1, 4, 8, MP, MQ>;
+template <bool MP, bool MQ> using Slots64 = GemmShape<4, 1, 4, 4, MP, MQ>;
+template <bool MP, bool MQ> using Slots32 = GemmShape<4, 1, 4, 2, MP, MQ>;
 
 static int slot_tile(int n_q) { return n_q <= 32 ? 32 : n_q <= 64 ? 64 : n_q <= 128 ? 128 : 256; }
 
