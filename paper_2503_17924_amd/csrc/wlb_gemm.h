@@ -421,8 +421,10 @@ struct Gemm {
 
     // Rows of output through LDS, so that memory sees whole 256-byte pieces: 32 rows n at a time (16 where there are no more), `Bytes` = 2 (bf16: all of the
     // wavefront's values of a row) or 4 (fp32: up to 64 of them).  value(i, j, r) gives the values; put(n, m, bits) takes 16 bytes: n, m counted in the tile.
-    template <int Bytes, class V, class Put>
-    __device__ __forceinline__ void rows_out(uint32_t room, V value, Put put) {
+    // mend(j, set): before a bf16 block j leaves, the lane may set(m, value) of its row n = lane % 16, m counted in the wavefront's part.
+    struct NoMend { template <class Set> __device__ __forceinline__ void operator()(int, Set) const {} };
+    template <int Bytes, class V, class Put, class Mend = NoMend>
+    __device__ __forceinline__ void rows_out(uint32_t room, V value, Put put, Mend mend = Mend{}) {
         constexpr int MOST = 256 / (16 * Bytes), G = S::BM < MOST ? S::BM : MOST, H = S::BN < 2 ? S::BN : 2;    // blocks of 16 m, of 16 n at a time
         constexpr int ROWB = G * 16 * Bytes, CH = ROWB / 16, RPI = 64 / CH;                      // bytes, chunks of a row; rows per pass
         static_assert(S::BM % G == 0 && S::BN % H == 0 && ROWB <= 256 && 16 * H % RPI == 0, "8 KiB of a wavefront");
@@ -442,6 +444,14 @@ struct Gemm {
                         else *reinterpret_cast<WLB_LDS f32x4*>((uintptr_t)to) = f32x4{v0, v1, v2, v3};
                         if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);      // few values out of the accumulators at a time
                     }
+                if (Bytes == 2 && G == S::BM) {
+#pragma unroll
+                    for (int j = 0; j < H; ++j)
+                        mend(j0 + j, [&](int m, float v) __attribute__((always_inline)) {
+                            const int row = j * 16 + lane % 16;
+                            *reinterpret_cast<WLB_LDS __bf16*>((uintptr_t)(mine + row * ROWB + (((m * 2 / 16) ^ (row & (CH - 1))) * 16) + m * 2 % 16)) = (__bf16)v;
+                        });
+                }
                 wait_lds();
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll

@@ -236,32 +236,42 @@ struct StatsDone {
         float2* s_part = (float2*)(smem + (room - g.lds));                    // [WM][TN]
         auto block = [&](int j, auto edge) __attribute__((always_inline)) {   // edge: words of the tile lie past the end
             const int n = g.wn * (S::BN * 16) + j * 16 + g.lane % 16;
-            auto logit = [&](int i, int r) __attribute__((always_inline)) {
-                const float l = g.sum(i, j, r);
-                return edge && first + i * 16 + r >= a.vocab ? -INFINITY : l;
-            };
+            float logit[S::BM][4];
+#pragma unroll
+            for (int i = 0; i < S::BM; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float l = g.sum(i, j, r);
+                    logit[i][r] = edge && first + i * 16 + r >= a.vocab ? -INFINITY : l;
+                }
             const int word = of_row(ahead.target, j, g.lane), t = word < 0 ? -1 : word - first;    // register that holds the target, if this lane has it
             float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
             for (int i = 0; i < S::BM; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) most[r] = fmaxf(most[r], logit(i, r));
+                for (int r = 0; r < 4; ++r) most[r] = fmaxf(most[r], logit[i][r]);
             float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, xhalf(top));
             if (__any(t >= 0 && t < S::BM * 16)) {
+                float l = 0.f;
+                bool mine = false;
 #pragma unroll
                 for (int i = 0; i < S::BM; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (t == i * 16 + r) a.target_logit[n0 + n] = g.sum(i, j, r);
+                    for (int r = 0; r < 4; ++r) {
+                        const bool here = t == i * 16 + r;
+                        l = here ? logit[i][r] : l;
+                        mine |= here;
+                    }
+                if (mine) a.target_logit[n0 + n] = l;
             }
             const float ref = top == -INFINITY ? -INFINITY : top * a.c2, from = top == -INFINITY ? 0.f : ref;    // a wavefront all of whose words lie past the end
             float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < S::BM; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) sum[r] += fast_exp2(__builtin_fmaf(logit(i, r), a.c2, -from));
+                for (int r = 0; r < 4; ++r) sum[r] += fast_exp2(__builtin_fmaf(logit[i][r], a.c2, -from));
             float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
             all += __shfl_xor(all, 16);
             all += xhalf(all);
@@ -427,18 +437,35 @@ struct DDone {
         for (int j = 0; j < S::BN; ++j) {
             lse2[j] = of_row(h.lse2, j, g.lane) * kLog2e;
             weight[j] = of_row(h.weight, j, g.lane);
-            target[j] = of_row(h.target, j, g.lane) - a.piece0 - first;
+            target[j] = of_row(h.target, j, g.lane) - a.piece0 - first;         // register that holds the target, if this lane has it
         }
-        auto out = [&](auto edge) __attribute__((always_inline)) {          // edge: words of the tile lie past the end, D is 0 there
+        auto share = [&](float l, int j) __attribute__((always_inline)) { return fast_exp2(__builtin_fmaf(l, a.c2, -lse2[j])); };
+        // edge: words of the tile lie past the end, D is 0 there
+        auto out = [&](auto edge) __attribute__((always_inline)) {
             g.template rows_out<2>(
                 room,
                 [&](int i, int j, int r) __attribute__((always_inline)) {
-                    const int word = i * 16 + r;
-                    const float e = fast_exp2(__builtin_fmaf(g.sum(i, j, r), a.c2, -lse2[j])), p = edge && first + word >= a.piece_n ? 0.f : e;
-                    return weight[j] * (target[j] == word ? p - 1.f : p);
+                    const float e = weight[j] * share(g.sum(i, j, r), j);
+                    return edge && first + i * 16 + r >= a.piece_n ? 0.f : e;
                 },
                 [&](int n, int m, const i32x4& v) __attribute__((always_inline)) {
                     if (n0 + n < w.qn) *reinterpret_cast<i32x4*>(a.d + (size_t)(n0 + n) * a.pitch + m0 + m) = v;
+                },
+                // the few targets among the words, from the unrounded probability (comparing every word with its row's target took 2.7 us a tile)
+                [&](int j, auto set) __attribute__((always_inline)) {
+                    const int t = target[j];
+                    if (!__any(t >= 0 && t < S::BM * 16)) return;
+                    float l = 0.f;
+                    bool mine = false;
+#pragma unroll
+                    for (int i = 0; i < S::BM; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const bool here = t == i * 16 + r;
+                            l = here ? g.sum(i, j, r) : l;
+                            mine |= here;
+                        }
+                    if (mine) set(t + (g.lane / 16) * 4, weight[j] * (share(l, j) - 1.f));
                 });
         };
         if (m0 + S::TM > a.piece_n) out(std::true_type{});
