@@ -73,11 +73,85 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(const int32_t* tokens, c
 }
 
 // ------------------------------------------------------------------------------------------
-// Sort of the slots by word: least significant digit first, every pass stable, so slots of one word stay in order and the
-// sums over them are reproducible.  Slots without a word get the key `vocab` and end up last.
+// Sort of the slots by word, stable: slots of one word stay in order and the sums over them are reproducible.  Slots without a word get
+// the key `vocab` and end up last.
+//
+// Up to kSearchMost slots: a slot's place is the number of slots that come before it.  Tiles of 256 slots are sorted by comparing all with
+// all, then every slot finds its place among each tile's words by a binary search, on the whole GPU (16408 slots: 18 us in all; one workgroup sorting by
+// digits took 38 us for half as many).  Above that digit by digit, three launches a pass (16408 slots: 45 us in all, nearly the same for twice as many).
+constexpr int kSearchMost = 131072, kSearchTile = 256, kSearchGroup = 16;       // tiles that a workgroup searches
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kDigitBits = 9;
-constexpr int kSortSmallRounds = 16;                            // one workgroup sorts up to 16 * 1024 slots in LDS
-constexpr int kSortBlock = 4 * kSortThreads;                    // slots per workgroup of the general sort
+constexpr int kSortBlock = 4 * kSortThreads;                    // slots per workgroup of the sort by digits
+
+struct SortArgs {
+    const int32_t *tokens, *q_idx;
+    int32_t *word[2], *slot[2];     // the sorted list ends up in [0]; [1]: ping-pong, or words by tile, sorted, and slots' places in their tile
+    uint32_t* hist;                 // by digits: [bins][blocks] of a pass; by search: [blocks][n_q] slots of a group of tiles that come before
+    int n_q, t_kv, vocab, passes, bits, blocks;
+};
+
+// Four threads to a slot, each compares it with a quarter of its tile.
+__global__ void __launch_bounds__(4 * kSearchTile) sort_tile_kernel(SortArgs a) {
+    __shared__ __attribute__((aligned(16))) int s_key[kSearchTile];
+    __shared__ int s_count[3][kSearchTile];
+    const int tid = threadIdx.x % kSearchTile, quarter = threadIdx.x / kSearchTile, i = (int)blockIdx.x * kSearchTile + tid;
+    if (quarter == 0) s_key[tid] = i < a.n_q ? slot_word(a.tokens, a.q_idx, i, a.t_kv, a.vocab, a.vocab) : 0x7ffffffe;
+    __syncthreads();
+    const int key = s_key[tid], j0 = quarter * (kSearchTile / 4);
+    // j comes before i: its word is smaller, or the same and j < i
+    int count = 0;
+#pragma unroll
+    for (int j = 0; j < kSearchTile / 4; j += 4) {
+        const int4 other = *reinterpret_cast<const int4*>(s_key + j0 + j);
+        const int ahead = tid - (j0 + j);
+        count += (other.x < key + (ahead > 0)) + (other.y < key + (ahead > 1)) + (other.z < key + (ahead > 2)) + (other.w < key + (ahead > 3));
+    }
+    if (quarter > 0) s_count[quarter - 1][tid] = count;
+    __syncthreads();
+    if (quarter > 0) return;
+    count += s_count[0][tid] + s_count[1][tid] + s_count[2][tid];
+    a.word[1][(int)blockIdx.x * kSearchTile + count] = key;
+    if (i < a.n_q) a.slot[1][i] = count;
+}
+
+__global__ void __launch_bounds__(kSearchTile) sort_search_kernel(SortArgs a) {
+    __shared__ __attribute__((aligned(16))) int s_key[kSearchGroup * kSearchTile];
+    const int tiles = (a.n_q + kSearchTile - 1) / kSearchTile, t0 = (int)blockIdx.y * kSearchGroup, nt = min(kSearchGroup, tiles - t0);
+    const int tid = threadIdx.x, own = blockIdx.x, i = own * kSearchTile + tid;
+    for (int c = tid; c < nt * (kSearchTile / 4); c += kSearchTile)
+        reinterpret_cast<int4*>(s_key)[c] = reinterpret_cast<const int4*>(a.word[1] + (size_t)t0 * kSearchTile)[c];
+    const int key = i < a.n_q ? slot_word(a.tokens, a.q_idx, i, a.t_kv, a.vocab, a.vocab) : 0;
+    int count = i < a.n_q && own >= t0 && own < t0 + nt ? a.slot[1][i] : 0;
+    __syncthreads();
+    // words below the slot's; of the tiles in front of its own, also the same word
+    constexpr int kAtOnce = 4;
+    for (int t = 0; t < nt; t += kAtOnce) {
+        int at[kAtOnce], limit[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            at[k] = 0;
+            limit[k] = t + k < nt && t0 + t + k != own ? key + (t0 + t + k < own) : -1;         // -1: none
+        }
+#pragma unroll
+        for (int step = kSearchTile / 2; step > 0; step /= 2)
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) at[k] += s_key[min(t + k, nt - 1) * kSearchTile + at[k] + step - 1] < limit[k] ? step : 0;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) count += at[k] + (s_key[min(t + k, nt - 1) * kSearchTile + at[k]] < limit[k]);
+    }
+    if (i < a.n_q) a.hist[(size_t)blockIdx.y * a.n_q + i] = count;
+}
+
+// Slots to their places.
+__global__ void __launch_bounds__(256) sort_place_kernel(SortArgs a) {
+    const int i = (int)(blockIdx.x * 256 + threadIdx.x);
+    if (i >= a.n_q) return;
+    uint32_t at = 0;
+#pragma unroll 8
+    for (int y = 0; y < a.blocks; ++y) at += a.hist[(size_t)y * a.n_q + i];
+    a.word[0][at] = slot_word(a.tokens, a.q_idx, i, a.t_kv, a.vocab, a.vocab);
+    a.slot[0][at] = i;
+}
 
 __device__ __forceinline__ uint32_t load_lds(const uint32_t* p) { return *(const volatile uint32_t*)p; }
 __device__ __forceinline__ void store_lds(uint32_t* p, uint32_t v) { *(volatile uint32_t*)p = v; }
@@ -129,64 +203,7 @@ __device__ __forceinline__ void scan_lds(uint32_t* v, int n, uint32_t* wave_sums
     __syncthreads();
 }
 
-struct SortArgs {
-    const int32_t *tokens, *q_idx;
-    int32_t *word[2], *slot[2];     // ping-pong; the sorted list ends up in [0]
-    uint32_t* hist;                 // [bins][blocks] of a pass
-    int32_t* n_valid;               // slots that hold a word
-    int n_q, t_kv, vocab, passes, bits, blocks;
-};
-
-// All passes in one workgroup: keys stay in registers and move through LDS.
-template <int R>
-__global__ void __launch_bounds__(kSortThreads) sort_small_kernel(SortArgs a) {
-    constexpr int N = R * kSortThreads;
-    __shared__ uint32_t s_key[N];
-    __shared__ uint16_t s_slot[N];
-    __shared__ uint32_t s_count[kSortWaves << kDigitBits];
-    __shared__ uint32_t s_sums[kSortWaves];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, at0 = wave * (64 * R) + lane;
-    uint32_t key[R], slot[R], rank[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int i = at0 + r * 64;
-        slot[r] = i;
-        key[r] = i < a.n_q ? slot_word(a.tokens, a.q_idx, i, a.t_kv, a.vocab, a.vocab) : a.vocab;
-    }
-    const int bins = 1 << a.bits;
-    for (int pass = 0; pass < a.passes; ++pass) {
-        const int shift = pass * a.bits;
-        for (int i = threadIdx.x; i < bins * kSortWaves; i += kSortThreads) s_count[i] = 0;
-        __syncthreads();
-        rank_digits<R>(key, rank, s_count, shift, a.bits, wave, lane);
-        __syncthreads();
-        scan_lds(s_count, bins * kSortWaves, s_sums);
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const uint32_t to = s_count[((key[r] >> shift) & (bins - 1)) * kSortWaves + wave] + rank[r];
-            s_key[to] = key[r];
-            s_slot[to] = (uint16_t)slot[r];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            key[r] = s_key[at0 + r * 64];
-            slot[r] = s_slot[at0 + r * 64];
-        }
-    }
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int i = at0 + r * 64;
-        if (i >= a.n_q) continue;
-        a.word[0][i] = (int)key[r];
-        a.slot[0][i] = (int)slot[r];
-        const bool valid = key[r] < (uint32_t)a.vocab;
-        if (valid && (i + 1 == a.n_q || s_key[i + 1] >= (uint32_t)a.vocab)) *a.n_valid = i + 1;
-        if (i == 0 && !valid) *a.n_valid = 0;
-    }
-}
-
-// General sort, three launches a pass.  src: the list that the pass reads, -1 = the slots themselves.
+// Sort by digits, least significant first.  src: the list that the pass reads, -1 = the slots themselves.
 __device__ __forceinline__ int sort_key(const SortArgs& a, int src, int i) {
     if (i >= a.n_q) return a.vocab;
     return src < 0 ? slot_word(a.tokens, a.q_idx, i, a.t_kv, a.vocab, a.vocab) : a.word[src][i];
@@ -254,14 +271,6 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(SortArgs a, 
     }
 }
 
-__global__ void sort_count_kernel(SortArgs a) {
-    const int i = (int)(blockIdx.x * blockDim.x + threadIdx.x);
-    if (i >= a.n_q) return;
-    const bool valid = a.word[0][i] < a.vocab;
-    if (valid && (i + 1 == a.n_q || a.word[0][i + 1] >= a.vocab)) *a.n_valid = i + 1;
-    if (i == 0 && !valid) *a.n_valid = 0;
-}
-
 // ------------------------------------------------------------------------------------------
 // Sums over the sorted list.  It is cut into pieces of `piece` positions, and a wavefront takes one piece and 512 columns (16 bytes a
 // lane): every wavefront has the same work however often a word occurs.  The sum of a word that lies within
@@ -271,11 +280,11 @@ __global__ void sort_count_kernel(SortArgs a) {
 constexpr int kSumUnroll = 8, kFillRows = 16;
 
 struct SumArgs {
-    const int32_t *word, *slot, *n_valid;
+    const int32_t *word, *slot;
     const uint4* dx;
     uint4* dtable;
     float4* part;            // [pieces][2][chunks][2]: partial sums, 8 floats a chunk of 16 bytes of bf16
-    int vocab, chunks, strips, piece, pieces, add;
+    int n_q, vocab, chunks, strips, piece, pieces, add;
     int sum_blocks;          // workgroups that sum; the others fill absent rows with zeros
     float scale;
 };
@@ -316,7 +325,7 @@ __device__ __forceinline__ void put_part(const SumArgs& a, int piece, int last, 
 }
 
 __global__ void __launch_bounds__(256) embed_sum_kernel(SumArgs a) {
-    const int wave = uniform((int)threadIdx.x >> 6), lane = threadIdx.x & 63, n = *a.n_valid;
+    const int wave = uniform((int)threadIdx.x >> 6), lane = threadIdx.x & 63, n = a.n_q;
     if ((int)blockIdx.x >= a.sum_blocks) {
         const int row0 = (((int)blockIdx.x - a.sum_blocks) * 4 + wave) * kFillRows, row = row0 + lane;
         bool absent = false;
@@ -334,11 +343,13 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(SumArgs a) {
         return;
     }
     const int task = (int)blockIdx.x * 4 + wave, piece = task / a.strips, c = (task - piece * a.strips) * 64 + lane;
-    const int p0 = piece * a.piece, count = min(a.piece, n - p0);
-    if (piece >= a.pieces || count <= 0) return;
+    const int p0 = piece * a.piece;
+    if (piece >= a.pieces) return;
     const bool on = c < a.chunks;
     const int at = min(p0 + lane, n - 1);
     const int my_word = a.word[at], my_slot = a.slot[at];
+    const int count = __popcll(__ballot(lane < a.piece && p0 + lane < n && my_word < a.vocab));      // the slots without a word stand at the end
+    if (count == 0) return;
     const int before = p0 > 0 ? a.word[p0 - 1] : -1, behind = p0 + count < n ? a.word[p0 + count] : -1;
     float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     bool began = before != __builtin_amdgcn_readlane(my_word, 0);       // the current word's first slot lies in this piece
@@ -376,37 +387,48 @@ __global__ void __launch_bounds__(256) embed_sum_kernel(SumArgs a) {
     }
 }
 
-// Sums that cross pieces: a wavefront per piece whose last word begins there and goes on, and 512 columns.
+// Sums that cross pieces: a workgroup per piece whose last word begins there and goes on, and 512 columns; each wavefront adds up a quarter of the
+// word's partial sums.
 __global__ void __launch_bounds__(256) embed_join_kernel(SumArgs a) {
-    const int wave = uniform((int)threadIdx.x >> 6), lane = threadIdx.x & 63, n = *a.n_valid;
-    const int task = (int)blockIdx.x * 4 + wave, piece = task / a.strips, c = (task - piece * a.strips) * 64 + lane;
+    __shared__ float s_sum[3][8][64];
+    const int wave = uniform((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int piece = (int)blockIdx.x / a.strips, c = ((int)blockIdx.x - piece * a.strips) * 64 + lane;
     const int p0 = piece * a.piece, p1 = p0 + a.piece;
-    if (piece >= a.pieces || p1 >= n) return;
+    if (p1 >= a.n_q) return;
     const int word = a.word[p1 - 1];
-    if (a.word[p1] != word || (p0 > 0 && a.word[p0 - 1] == word)) return;
-    const int last = uniform((lower_bound(a.word, n, word + 1) - 1) / a.piece);         // piece that holds the word's last slot
-    if (c >= a.chunks) return;
+    if (word >= a.vocab || a.word[p1] != word || (p0 > 0 && a.word[p0 - 1] == word)) return;
+    const int last = uniform((lower_bound(a.word, a.n_q, word + 1) - 1) / a.piece);     // piece that holds the word's last slot
+    const int first = piece + 1 + (int)((long long)(last - piece) * wave / 4), end = piece + 1 + (int)((long long)(last - piece) * (wave + 1) / 4);
+    const bool on = c < a.chunks;
     float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     auto add = [&](const float4& u, const float4& v) __attribute__((always_inline)) {
         s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
         s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
     };
-    const float4* from = a.part + ((size_t)(2 * piece + 1) * a.chunks + c) * 2;
-    add(from[0], from[1]);
-    const size_t step = (size_t)4 * a.chunks;                   // float4 between the partial sums of two pieces
-    from = a.part + ((size_t)(2 * (piece + 1)) * a.chunks + c) * 2;
-    for (int p = piece + 1; p <= last; p += kSumUnroll) {
+    auto part = [&](int p, int which) __attribute__((always_inline)) { return a.part + ((size_t)(2 * p + which) * a.chunks + (on ? c : 0)) * 2; };
+    if (wave == 0) add(part(piece, 1)[0], part(piece, 1)[1]);
+    for (int p = first; p < end; p += kSumUnroll) {
         float4 u[kSumUnroll], v[kSumUnroll];
 #pragma unroll
         for (int k = 0; k < kSumUnroll; ++k) {
-            const size_t at = (size_t)(min(p + k, last) - (piece + 1)) * step;
-            u[k] = from[at];
-            v[k] = from[at + 1];
+            const float4* from = part(min(p + k, end - 1), 0);
+            u[k] = from[0];
+            v[k] = from[1];
         }
 #pragma unroll
         for (int k = 0; k < kSumUnroll; ++k)
-            if (p + k <= last) add(u[k], v[k]);
+            if (p + k < end) add(u[k], v[k]);
     }
+    if (wave > 0) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s_sum[wave - 1][k][lane] = s[k];
+    }
+    __syncthreads();
+    if (wave > 0 || !on) return;
+#pragma unroll
+    for (int w = 0; w < 3; ++w)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s[k] += s_sum[w][k][lane];
     put_row(a, word, c, s);
 }
 
@@ -419,9 +441,9 @@ static int sum_piece(const wlb_vocab_desc& d) {
 }
 
 struct EmbedLayout {
-    size_t off_word[2], off_slot[2], off_hist, off_valid, off_part, bytes;
+    size_t off_word[2], off_slot[2], off_hist, off_part, bytes;
     int passes, bits, blocks, piece, pieces;
-    bool small;
+    bool search;                     // sorted by search, `blocks` groups of tiles
 };
 
 static EmbedLayout embed_layout(const wlb_vocab_desc& d) {
@@ -430,19 +452,19 @@ static EmbedLayout embed_layout(const wlb_vocab_desc& d) {
     while (((unsigned)d.vocab >> bits) != 0) ++bits;             // keys 0 .. vocab
     L.passes = (bits + kDigitBits - 1) / kDigitBits;
     L.bits = (bits + L.passes - 1) / L.passes;
-    L.small = d.n_q <= kSortSmallRounds * kSortThreads;
-    L.blocks = L.small ? 0 : (d.n_q + kSortBlock - 1) / kSortBlock;
+    L.search = d.n_q <= kSearchMost;
+    const int per = L.search ? kSearchTile * kSearchGroup : kSortBlock;
+    L.blocks = (d.n_q + per - 1) / per;
     L.piece = sum_piece(d);
     L.pieces = (d.n_q + L.piece - 1) / L.piece;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
     for (int i = 0; i < 2; ++i) {
-        const size_t list = i == 0 || !L.small ? sizeof(int32_t) * (size_t)d.n_q : 0;
+        const size_t list = sizeof(int32_t) * align_up(d.n_q, kSearchTile);
         L.off_word[i] = take(list);
         L.off_slot[i] = take(list);
     }
-    L.off_hist = take(sizeof(uint32_t) * ((size_t)L.blocks << L.bits));
-    L.off_valid = take(sizeof(int32_t));
+    L.off_hist = take(sizeof(uint32_t) * (L.search ? (size_t)L.blocks * d.n_q : (size_t)L.blocks << L.bits));
     L.off_part = take(sizeof(float) * 2 * (size_t)L.pieces * d.hidden);
     L.bytes = at;
     return L;
@@ -489,12 +511,12 @@ extern "C" wlb_status wlb_embed_bwd(const wlb_vocab_desc* desc, const int32_t* t
         s.slot[i] = (int32_t*)(ws + L.off_slot[i]);
     }
     s.hist = (uint32_t*)(ws + L.off_hist);
-    s.n_valid = (int32_t*)(ws + L.off_valid);
     s.n_q = d.n_q; s.t_kv = d.t_kv; s.vocab = d.vocab; s.passes = L.passes; s.bits = L.bits; s.blocks = L.blocks;
-    if (L.small) {
-        if (d.n_q <= kSortThreads) sort_small_kernel<1><<<1, kSortThreads, 0, stream>>>(s);
-        else if (d.n_q <= 4 * kSortThreads) sort_small_kernel<4><<<1, kSortThreads, 0, stream>>>(s);
-        else sort_small_kernel<kSortSmallRounds><<<1, kSortThreads, 0, stream>>>(s);
+    if (L.search) {
+        const int tiles = (d.n_q + kSearchTile - 1) / kSearchTile;
+        sort_tile_kernel<<<tiles, 4 * kSearchTile, 0, stream>>>(s);
+        sort_search_kernel<<<dim3(tiles, L.blocks), kSearchTile, 0, stream>>>(s);
+        sort_place_kernel<<<(d.n_q + 255) / 256, 256, 0, stream>>>(s);
     } else {
         int src = -1;
         for (int pass = 0; pass < L.passes; ++pass) {
@@ -504,17 +526,16 @@ extern "C" wlb_status wlb_embed_bwd(const wlb_vocab_desc* desc, const int32_t* t
             sort_scatter_kernel<<<L.blocks, kSortThreads, 0, stream>>>(s, src, dst, shift);
             src = dst;
         }
-        sort_count_kernel<<<(d.n_q + 255) / 256, 256, 0, stream>>>(s);
     }
     SumArgs a;
-    a.word = s.word[0]; a.slot = s.slot[0]; a.n_valid = s.n_valid;
+    a.word = s.word[0]; a.slot = s.slot[0]; a.n_q = d.n_q;
     a.dx = (const uint4*)dx; a.dtable = (uint4*)dtable; a.part = (float4*)(ws + L.off_part);
     a.vocab = d.vocab; a.chunks = d.hidden / 8; a.strips = (a.chunks + 63) / 64;
     a.piece = L.piece; a.pieces = L.pieces; a.add = d.flags & WLB_VOCAB_ACCUMULATE; a.scale = d.scale;
     a.sum_blocks = (int)(((long long)a.pieces * a.strips + 3) / 4);
     const int fill_blocks = a.add ? 0 : (d.vocab + 4 * kFillRows - 1) / (4 * kFillRows);
     embed_sum_kernel<<<a.sum_blocks + fill_blocks, 256, 0, stream>>>(a);
-    if (a.pieces > 1) embed_join_kernel<<<a.sum_blocks, 256, 0, stream>>>(a);
+    if (a.pieces > 1) embed_join_kernel<<<(unsigned)a.pieces * a.strips, 256, 0, stream>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(WLB_ERR_HIP, "lookup gradient launch: %s", hipGetErrorString(e));
     return WLB_OK;

@@ -465,10 +465,10 @@ struct Gemm {
             }
     }
 
-    // the partial sums of a divided tile: [TN][256] floats
-    __device__ __forceinline__ void part_out(uint32_t room, float* to) {
+    // the partial sums of a divided tile: [TN][256] floats, of which `rows` are read
+    __device__ __forceinline__ void part_out(uint32_t room, float* to, int rows) {
         rows_out<4>(room, [&](int i, int j, int r) __attribute__((always_inline)) { return sum(i, j, r); },
-                    [&](int n, int m, const i32x4& v) __attribute__((always_inline)) { *reinterpret_cast<i32x4*>(to + n * S::TM + m) = v; });
+                    [&](int n, int m, const i32x4& v) __attribute__((always_inline)) { if (n < rows) *reinterpret_cast<i32x4*>(to + n * S::TM + m) = v; });
     }
 };
 

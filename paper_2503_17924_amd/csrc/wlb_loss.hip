@@ -162,25 +162,37 @@ struct Work : GemmGrid {
     }
 };
 
-// Joins the parts of divided tiles in order: f(tm, tn, n, m, four sums), a wavefront to a row n of a tile.
+// Joins the parts of divided tiles in order: f(tm, tn, n, m, four sums).  A row n of a tile is a wavefront's, of a narrow tile, which has up to kMaxParts parts, a
+// workgroup's, whose wavefronts add up a quarter of the parts each.
+template <class S> constexpr int join_rows() { return S::RING ? 4 : 1; }        // rows of a tile to a workgroup
 template <class S, class F>
 __device__ __forceinline__ void join_parts(const Work& w, const float* parts, F f) {
     static_assert(S::TM == 256, "four columns a lane");
-    const int lane = threadIdx.x & 63, id = uniform((int)blockIdx.x * 4 + ((int)threadIdx.x >> 6));
+    __shared__ f32x4 s_sum[3][64];
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), id = S::RING ? (int)blockIdx.x * 4 + wave : (int)blockIdx.x;
     GemmItem it;
     if (id >= w.left * S::TN) return;
     w.place(w.whole + id / S::TN, it);
     const int n = id % S::TN;
+    if (it.tn * S::TN + n >= w.qn) return;
+    const int first = S::RING ? 0 : w.parts * wave / 4, end = S::RING ? w.parts : w.parts * (wave + 1) / 4;
     const f32x4* from = reinterpret_cast<const f32x4*>(parts + ((size_t)(id / S::TN) * w.parts * S::TN + n) * S::TM) + lane;
     f32x4 sum = {0, 0, 0, 0};
     constexpr int kAhead = 8;
-    for (int k = 0; k < w.parts; k += kAhead) {
+    for (int k = first; k < end; k += kAhead) {
         f32x4 v[kAhead];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) v[i] = from[(size_t)min(k + i, w.parts - 1) * (S::TN * S::TM / 4)];
+        for (int i = 0; i < kAhead; ++i) v[i] = from[(size_t)min(k + i, end - 1) * (S::TN * S::TM / 4)];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i)
-            if (k + i < w.parts) sum += v[i];
+            if (k + i < end) sum += v[i];
+    }
+    if (!S::RING) {
+        if (wave > 0) s_sum[wave - 1][lane] = sum;
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) sum += s_sum[i][lane];
     }
     f(it.tm, it.tn, n, lane * 4, sum);
 }
@@ -228,7 +240,7 @@ struct StatsDone {
     }
     __device__ __forceinline__ void operator()(Gemm<S>& g, const GemmItem& it, const Ahead& ahead, uint32_t room) const {
         if (it.part >= 0) {
-            g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN));
+            g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN), w.qn - it.tn * S::TN);
             return;
         }
         const int m0 = it.tm * S::TM, n0 = it.tn * S::TN, n_rows = w.qn;
@@ -426,7 +438,7 @@ struct DDone {
     }
     __device__ __forceinline__ void operator()(Gemm<S>& g, const GemmItem& it, const Ahead& h, uint32_t room) const {
         if (it.part >= 0) {
-            g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN));
+            g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN), w.qn - it.tn * S::TN);
             return;
         }
         const int m0 = it.tm * S::TM, n0 = it.tn * S::TN;
@@ -514,11 +526,12 @@ struct NothingAhead {
 template <class S>
 struct DtableDone : NothingAhead {
     const GradArgs& a;
+    const Work& w;
     float factor;
-    __device__ __forceinline__ DtableDone(const GradArgs& a_) : a(a_), factor(*a_.factor) {}
+    __device__ __forceinline__ DtableDone(const GradArgs& a_, const Work& w_) : a(a_), w(w_), factor(*a_.factor) {}
     __device__ __forceinline__ void operator()(Gemm<S>& g, const GemmItem& it, Ahead, uint32_t room) const {
         if (it.part >= 0) {
-            g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN));
+            g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN), w.qn - it.tn * S::TN);
             return;
         }
         const int m0 = it.tm * S::TM, n0 = it.tn * S::TN;
@@ -535,7 +548,7 @@ __global__ void __launch_bounds__(256, S::PER_CU) loss_dtable_kernel(GradArgs a)
     __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
     const Work w = dtable_work<S>(a);
     Gemm<S> gemm;
-    gemm.run(smem, w, DtableDone<S>(a));
+    gemm.run(smem, w, DtableDone<S>(a, w));
 }
 
 template <class S>
@@ -571,7 +584,7 @@ struct DxDone : NothingAhead {
     __device__ __forceinline__ DxDone(const GradArgs& a_, const Work& w_) : a(a_), w(w_), factor(*a_.factor) {}
     __device__ __forceinline__ void operator()(Gemm<S>& g, const GemmItem& it, Ahead, uint32_t room) const {
         if (it.part >= 0) {
-            g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN));
+            g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN), w.qn - it.tn * S::TN);
             return;
         }
         const int m0 = it.tm * S::TM, n0 = it.tn * S::TN;
@@ -604,6 +617,10 @@ template <bool MP, bool MQ> using Half = GemmShape<2, 2, 4, 4, MP, MQ>;
 template <bool MP, bool MQ> using Slots128 = GemmShape<4, 1, 4, 8, MP, MQ>;
 template <bool MP, bool MQ> using Slots64 = GemmShape<4, 1, 4, 4, MP, MQ>;
 template <bool MP, bool MQ> using Slots32 = GemmShape<4, 1, 4, 2, MP, MQ>;
+// the same with tiles of 128 words
+using Slots128Low = GemmShape<4, 1, 2, 8, false, false>;
+using Slots64Low = GemmShape<4, 1, 2, 4, false, false>;
+using Slots32Low = GemmShape<4, 1, 2, 2, false, false>;
 
 static int slot_tile(int n_q) { return n_q <= 32 ? 32 : n_q <= 64 ? 64 : n_q <= 128 ? 128 : 256; }
 
@@ -613,15 +630,15 @@ constexpr size_t kPieceBytes = 512u << 20;
 constexpr int kPieceMin = 16384;
 
 static unsigned tile_grid(long long tiles) { return (unsigned)((tiles + kLists - 1) / kLists * kLists); }
-// Workgroups of a launch of wide tiles (one to a compute unit) and of a product that narrow tiles divide along k (two).
+// Workgroups of a launch of wide tiles, and of a product that narrow tiles divide along k: one to a compute unit (two, with twice as many parts, took
+// longer: dX of 65 slots, 32768 words, hidden 1024, and its join 37 us, with one 27).
 static int wide_workgroups() { return std::max(kLists, compute_units() / kLists * kLists); }
-static int narrow_workgroups() { return 2 * wide_workgroups(); }
 
 struct LossLayout {
     size_t off_count, off_factor, off_slot_target, off_block_count, off_block_max, off_rows, off_target, off_row_lse, off_row_weight, off_parts;
     size_t off_part, off_target_logit, fwd_bytes;                 // forward
     size_t off_rows_x, off_d, off_dx_sum, bwd_bytes;              // backward
-    int blocks, tile, word_tiles, pitch_rows, piece, pieces;
+    int blocks, tile, word_tile, word_tiles, pitch_rows, piece, pieces;
 };
 
 static LossLayout loss_layout(const wlb_vocab_desc& d) {
@@ -629,7 +646,9 @@ static LossLayout loss_layout(const wlb_vocab_desc& d) {
     const size_t n_q = d.n_q, v = d.vocab, h = d.hidden;
     L.blocks = (d.n_q + kRowsThreads - 1) / kRowsThreads;
     L.tile = slot_tile(d.n_q);
-    L.word_tiles = (d.vocab + kWordTile - 1) / kWordTile;
+    // Few slots: tiles of 128 words where those of 256 are fewer than the compute units (32768 words, 33 slots, hidden 1024: statistics 14.4 us, with 256 18.6)
+    L.word_tile = L.tile < 256 && (d.vocab + kWordTile - 1) / kWordTile < compute_units() ? kWordTile / 2 : kWordTile;
+    L.word_tiles = (d.vocab + L.word_tile - 1) / L.word_tile;
     L.pitch_rows = (int)align_up(n_q, 64);
     const size_t words = align_up(v, kWordTile);
     size_t piece = std::max((size_t)kPieceMin, kPieceBytes / (2 * n_q) / kWordTile * kWordTile);
@@ -647,7 +666,7 @@ static LossLayout loss_layout(const wlb_vocab_desc& d) {
     L.off_row_lse = take(4 * n_q);
     L.off_row_weight = take(4 * n_q);
     // a divided tile's parts are no more than the workgroups of the launch
-    L.off_parts = take(sizeof(float) * kWordTile * (size_t)L.tile * (L.tile < 256 ? narrow_workgroups() : wide_workgroups()));
+    L.off_parts = take(sizeof(float) * kWordTile * (size_t)L.tile * wide_workgroups());
     const size_t common = at;
     L.off_part = take(sizeof(float2) * (size_t)L.word_tiles * L.pitch_rows);
     L.off_target_logit = take(4 * n_q);
@@ -668,7 +687,7 @@ static wlb_status check_loss(const wlb_vocab_desc* desc, const char* call) {
     // rows of x are addressed with 32-bit offsets
     if ((uint64_t)desc->n_q * desc->hidden * 2 >= (1ull << 32) - (1u << 20))
         return fail(WLB_ERR_UNSUPPORTED, "%s: x of 4 GiB or more is not supported", call);
-    if ((int64_t)(desc->vocab / kWordTile + 1) * (desc->n_q / 32 + 1) > (1 << 30))
+    if ((int64_t)(desc->vocab / (kWordTile / 2) + 1) * (desc->n_q / 32 + 1) > (1 << 30))
         return fail(WLB_ERR_UNSUPPORTED, "%s: vocab=%d words for n_q=%d slots", call, desc->vocab, desc->n_q);
     return WLB_OK;
 }
@@ -716,9 +735,9 @@ static void launch_narrow(K kernel, A& a, long long tiles, hipStream_t stream) {
 // Narrow tiles along the columns, all divided along the words.  tile: slots of one
 template <class K, class J, class A>
 static void launch_divided(K kernel, J join, A& a, int tile, int tiles, hipStream_t stream) {
-    a.workgroups = narrow_workgroups();
+    a.workgroups = wide_workgroups();
     kernel<<<a.workgroups, 256, 0, stream>>>(a);
-    join<<<std::min(tiles, a.workgroups / 2) * tile / 4, 256, 0, stream>>>(a);
+    join<<<std::min(tiles, a.workgroups / 2) * tile, 256, 0, stream>>>(a);
 }
 
 }  // namespace wlb
@@ -754,9 +773,10 @@ extern "C" wlb_status wlb_loss_fwd(const wlb_vocab_desc* desc, const void* x, co
     a.part = (float2*)(ws + L.off_part); a.target_logit = (float*)(ws + L.off_target_logit);
     a.vocab = d.vocab; a.hidden = d.hidden; a.pitch = L.pitch_rows; a.c2 = d.scale * kLog2e;
     a.parts = (float*)(ws + L.off_parts);
-    if (L.tile == 32) launch_narrow(loss_stats_kernel<Slots32<false, false>>, a, L.word_tiles, stream);
-    else if (L.tile == 64) launch_narrow(loss_stats_kernel<Slots64<false, false>>, a, L.word_tiles, stream);
-    else if (L.tile == 128) launch_narrow(loss_stats_kernel<Slots128<false, false>>, a, L.word_tiles, stream);
+    const bool low = L.word_tile < kWordTile;
+    if (L.tile == 32) launch_narrow(low ? loss_stats_kernel<Slots32Low> : loss_stats_kernel<Slots32<false, false>>, a, L.word_tiles, stream);
+    else if (L.tile == 64) launch_narrow(low ? loss_stats_kernel<Slots64Low> : loss_stats_kernel<Slots64<false, false>>, a, L.word_tiles, stream);
+    else if (L.tile == 128) launch_narrow(low ? loss_stats_kernel<Slots128Low> : loss_stats_kernel<Slots128<false, false>>, a, L.word_tiles, stream);
     else launch_wide(loss_stats_kernel<Wide<false, false>>, loss_stats_parts_kernel<Wide<false, false>>, a, d.hidden, stream);
     loss_join_kernel<<<(d.n_q + 31) / 32, 256, 0, stream>>>(a.part, a.target_logit, a.rows, a.count, loss, lse, L.word_tiles, L.pitch_rows, a.c2);
     hipError_t e = hipGetLastError();
@@ -788,18 +808,21 @@ extern "C" wlb_status wlb_loss_bwd(const wlb_vocab_desc* desc, const void* x, co
     a.vocab = d.vocab; a.hidden = d.hidden; a.n_q = d.n_q; a.pitch = L.piece; a.c2 = d.scale * kLog2e;
     loss_gather_kernel<<<(d.n_q + 3) / 4, 256, 0, stream>>>((const uint4*)x, (uint4*)a.rows_x, (uint4*)dx, a.rows, r.slot_target, a.count, d.n_q, d.hidden / 8);
     a.parts = (float*)(ws + L.off_parts);
+    const bool low = L.word_tile < kWordTile;
     for (int p = 0; p < L.pieces; ++p) {
         a.piece0 = p * L.piece;
         a.piece_n = std::min(L.piece, d.vocab - a.piece0);
         a.add = p > 0;
         a.final = p == L.pieces - 1;
         const int word_tiles = (a.piece_n + kWordTile - 1) / kWordTile, column_tiles = (d.hidden + kWordTile - 1) / kWordTile;
-        if (L.tile == 32) launch_narrow(loss_d_kernel<Slots32<false, false>>, a, word_tiles, stream);
-        else if (L.tile == 64) launch_narrow(loss_d_kernel<Slots64<false, false>>, a, word_tiles, stream);
-        else if (L.tile == 128) launch_narrow(loss_d_kernel<Slots128<false, false>>, a, word_tiles, stream);
+        const int few_tiles = (a.piece_n + L.word_tile - 1) / L.word_tile;
+        if (L.tile == 32) launch_narrow(low ? loss_d_kernel<Slots32Low> : loss_d_kernel<Slots32<false, false>>, a, few_tiles, stream);
+        else if (L.tile == 64) launch_narrow(low ? loss_d_kernel<Slots64Low> : loss_d_kernel<Slots64<false, false>>, a, few_tiles, stream);
+        else if (L.tile == 128) launch_narrow(low ? loss_d_kernel<Slots128Low> : loss_d_kernel<Slots128<false, false>>, a, few_tiles, stream);
         else launch_wide(loss_d_kernel<Wide<false, false>>, loss_d_parts_kernel<Wide<false, false>>, a, d.hidden, stream);
-        // tiles of 128 x 128 where wide ones neither fill the launch nor have rows enough to be divided
-        if ((long long)word_tiles * column_tiles >= wide_workgroups() || d.n_q >= 2 * kWideParts * kStepK)
+        // tiles of 128 x 128 where wide ones neither fill the launch nor have rows enough to be divided, and where there is but one step, in front of
+        // and behind which nothing runs beside a wide tile (33 slots, 65536 words, hidden 2048: 66 us, wide 71; 128 slots: 84 and 73)
+        if (d.n_q > kStepK && ((long long)word_tiles * column_tiles >= wide_workgroups() || d.n_q >= 2 * kWideParts * kStepK))
             launch_wide(loss_dtable_kernel<Wide<true, true>>, loss_dtable_parts_kernel<Wide<true, true>>, a, d.n_q, stream);
         else launch_narrow(loss_dtable_kernel<Half<true, true>>, a, (long long)((a.piece_n + 127) / 128) * ((d.hidden + 127) / 128), stream);
         if (L.tile == 32) launch_divided(loss_dx_kernel<Slots32<true, false>>, loss_dx_parts_kernel<Slots32<true, false>>, a, 32, column_tiles, stream);

@@ -132,10 +132,11 @@ def test_loss_and_its_gradient(docs, cp, rank, vocab, hidden):
     Ends(2, docs, cp, rank, vocab, hidden, 0.7).check_loss()
 
 
-@pytest.mark.parametrize("docs,vocab,hidden", [([16384], 3, 64), ([16385], 70000, 16), ([40000, 5], 600000, 8), ([30000], 5, 520), ([20000], 300, 1040)])
+@pytest.mark.parametrize("docs,vocab,hidden", [([4096], 3, 64), ([4097], 70000, 16), ([131072], 3, 8), ([131073], 70000, 16), ([140000, 5], 600000, 8),
+                                               ([30000], 5, 520), ([20000], 300, 1040), ([9000, 1], 2000, 8)])
 def test_lookup_gradient_of_many_slots(docs, vocab, hidden):
-    """The largest list that one workgroup sorts and the first that takes several; one to three digits; words that fill
-    hundreds of pieces."""
+    """One group of tiles and the first slot behind it; the largest list that is sorted by search and the first that is sorted by digits, one to
+    three of them; words that fill hundreds of pieces."""
     e = Ends(3, docs, 1, 0, vocab, hidden, 2.0)
     e.check_embed()
     e.check_embed_bwd()
