@@ -348,20 +348,22 @@ __global__ void __launch_bounds__(256) loss_stats_parts_kernel(StatsArgs a) {
     });
 }
 
-// A slot's tiles combined: 32 rows to a workgroup, 8 threads to a row.
+// A slot's tiles combined: R rows to a workgroup, 256 / R threads to a row (few rows have few workgroups, and more tiles).
+template <int R>
 __global__ void __launch_bounds__(256) loss_join_kernel(const float2* part, const float* target_logit, const int32_t* rows, const int32_t* count, float* loss,
                                                         float* lse, int tiles, int pitch, float c2) {
-    __shared__ float2 s_part[8][32];
-    const int n_rows = *count, x = threadIdx.x & 31, y = threadIdx.x >> 5, row = (int)blockIdx.x * 32 + x;
+    constexpr int W = 256 / R;
+    __shared__ float2 s_part[W][R];
+    const int n_rows = *count, x = threadIdx.x % R, y = threadIdx.x / R, row = (int)blockIdx.x * R + x;
     constexpr float kLn2 = 0.6931471805599453f;
-    if ((int)blockIdx.x * 32 >= n_rows) return;
+    if ((int)blockIdx.x * R >= n_rows) return;
     constexpr int kAhead = 8;
     float ref = -INFINITY, sum = 0.f;
     if (row < n_rows)
-        for (int t = y; t < tiles; t += 8 * kAhead) {
+        for (int t = y; t < tiles; t += W * kAhead) {
             float2 p[kAhead];
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) p[k] = t + 8 * k < tiles ? part[(size_t)(t + 8 * k) * pitch + row] : float2{-INFINITY, 0.f};
+            for (int k = 0; k < kAhead; ++k) p[k] = t + W * k < tiles ? part[(size_t)(t + W * k) * pitch + row] : float2{-INFINITY, 0.f};
             float r = ref;
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) r = fmaxf(r, p[k].x);
@@ -373,9 +375,9 @@ __global__ void __launch_bounds__(256) loss_join_kernel(const float2* part, cons
     s_part[y][x] = float2{ref, sum};
     __syncthreads();
     if (y != 0 || row >= n_rows) return;
-    for (int k = 1; k < 8; ++k) ref = fmaxf(ref, s_part[k][x].x);
+    for (int k = 1; k < W; ++k) ref = fmaxf(ref, s_part[k][x].x);
     sum = 0.f;
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < W; ++k) {
         const float2 p = s_part[k][x];
         sum += p.x == -INFINITY ? p.y : p.y * fast_exp2(p.x - ref);
     }
@@ -646,7 +648,7 @@ static LossLayout loss_layout(const wlb_vocab_desc& d) {
     const size_t n_q = d.n_q, v = d.vocab, h = d.hidden;
     L.blocks = (d.n_q + kRowsThreads - 1) / kRowsThreads;
     L.tile = slot_tile(d.n_q);
-    // Few slots: tiles of 128 words where those of 256 are fewer than the compute units (32768 words, 33 slots, hidden 1024: statistics 14.4 us, with 256 18.6)
+    // Few slots: tiles of 128 words where those of 256 are fewer than the compute units (32768 words, hidden 1024, 65 slots: statistics 19 us, with 256 33).
     L.word_tile = L.tile < 256 && (d.vocab + kWordTile - 1) / kWordTile < compute_units() ? kWordTile / 2 : kWordTile;
     L.word_tiles = (d.vocab + L.word_tile - 1) / L.word_tile;
     L.pitch_rows = (int)align_up(n_q, 64);
@@ -778,7 +780,8 @@ extern "C" wlb_status wlb_loss_fwd(const wlb_vocab_desc* desc, const void* x, co
     else if (L.tile == 64) launch_narrow(low ? loss_stats_kernel<Slots64Low> : loss_stats_kernel<Slots64<false, false>>, a, L.word_tiles, stream);
     else if (L.tile == 128) launch_narrow(low ? loss_stats_kernel<Slots128Low> : loss_stats_kernel<Slots128<false, false>>, a, L.word_tiles, stream);
     else launch_wide(loss_stats_kernel<Wide<false, false>>, loss_stats_parts_kernel<Wide<false, false>>, a, d.hidden, stream);
-    loss_join_kernel<<<(d.n_q + 31) / 32, 256, 0, stream>>>(a.part, a.target_logit, a.rows, a.count, loss, lse, L.word_tiles, L.pitch_rows, a.c2);
+    if (L.tile < 256) loss_join_kernel<4><<<(d.n_q + 3) / 4, 256, 0, stream>>>(a.part, a.target_logit, a.rows, a.count, loss, lse, L.word_tiles, L.pitch_rows, a.c2);
+    else loss_join_kernel<32><<<(d.n_q + 31) / 32, 256, 0, stream>>>(a.part, a.target_logit, a.rows, a.count, loss, lse, L.word_tiles, L.pitch_rows, a.c2);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(WLB_ERR_HIP, "loss launch: %s", hipGetErrorString(e));
     return WLB_OK;
