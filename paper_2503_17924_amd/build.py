@@ -27,6 +27,8 @@ FLAGS = [
 
 # Sources whose kernels use the accumulation registers by number, in statements marked "; acc"
 OWN_ACC_REGISTERS = ["wlb_attn_dkv.hip", "wlb_attn_fwd_pair.hip", "wlb_attn_dq_pair.hip"]
+# Sources whose assembly is checked for wait states around hand-written statements and for registers kept in memory
+CHECKED_ASM = [*OWN_ACC_REGISTERS, "wlb_loss.hip"]
 
 
 def check_acc_registers(asm: str) -> None:
@@ -152,10 +154,11 @@ def build(verbose: bool = False, keep_asm: bool = False, lib_out: str | None = N
             # results of MFMAs that the vector ALU reads stay out of the accumulation registers, which the kernels
             # of this file number themselves (check_acc_registers)
             cmd += ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
+        if src in CHECKED_ASM:
             # the assembly that is checked is the one that is linked (the source's own switch for this warning is lost on the way)
             cmd += ["-save-temps=obj", "-Wno-inline-asm"]
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, cwd=bdir)))
-        if keep_asm and src.endswith(".hip") and src not in OWN_ACC_REGISTERS:
+        if keep_asm and src.endswith(".hip") and src not in CHECKED_ASM:
             asm = [c for c in cmd if c != "-c"]
             asm[asm.index("-o") + 1] = os.path.join(bdir, os.path.splitext(src)[0] + ".s")
             asm += ["-S", "--cuda-device-only"]
@@ -168,9 +171,10 @@ def build(verbose: bool = False, keep_asm: bool = False, lib_out: str | None = N
             raise RuntimeError(f"hipcc failed on {src}:\n{out}")
         if verbose and out.strip():
             print(out)
-    for src in OWN_ACC_REGISTERS:
+    for src in CHECKED_ASM:
         asm = os.path.join(bdir, os.path.splitext(src)[0] + "-hip-amdgcn-amd-amdhsa-gfx950.s")
-        check_acc_registers(asm)
+        if src in OWN_ACC_REGISTERS:
+            check_acc_registers(asm)
         check_wait_states(asm)
         check_scratch(asm)
     tmp = lib_out + ".tmp"

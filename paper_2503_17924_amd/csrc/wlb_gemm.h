@@ -52,16 +52,24 @@ struct GemmItem {
 // XCD b % 8; each XCD takes a consecutive share of the tiles in bands of kBand tiles along n, so that the workgroups that run side by
 // side on it share kBand operand tiles along n and a few along m in its L2.
 constexpr int kBand = 8, kMaxParts = 128;
+// In steps: an item's end (its sums go out while nothing else runs), and what a part costs the join, with its write and read of 256 KiB, in tenths.
+constexpr int kEndSteps = 6, kJoinSteps = 4;
 struct GemmGrid {
     int ntm, ntn, depth, workgroups, whole, left, parts;
-    // part_steps: a divided tile's part has at least this many steps
-    __device__ __forceinline__ GemmGrid(int ntm_, int ntn_, int depth_, int workgroups_, int part_steps) : ntm(ntm_), ntn(ntn_), depth(depth_), workgroups(workgroups_) {
-        const int tiles = ntm * ntn, steps = (depth + kStepK - 1) / kStepK;
+    // part_steps: a divided tile's part has at least this many steps.  rounds: how many the parts may take; with one, tiles are divided wherever they can be,
+    // with more where it pays: 160 tiles of 512 steps on 256 workgroups take 518 steps, in 3 parts each 2 * (171 + 6) and the join's 52.
+    __device__ __forceinline__ GemmGrid(int ntm_, int ntn_, int depth_, int workgroups_, int part_steps, int rounds) : ntm(ntm_), ntn(ntn_), depth(depth_), workgroups(workgroups_) {
+        const int tiles = ntm * ntn, steps = (depth + kStepK - 1) / kStepK, most = min(kMaxParts, steps / part_steps);
         left = uniform(tiles % workgroups);
-        parts = left ? uniform(workgroups / left) : 1;
-        if (parts > kMaxParts) parts = kMaxParts;
-        if (parts > steps / part_steps) parts = steps / part_steps;
-        if (parts < 2) { parts = 1; left = 0; }
+        parts = 1;
+        int least = rounds > 1 ? steps + kEndSteps : 1 << 30;
+        for (int r = 1; left > 0 && r <= rounds; ++r) {
+            const int p = min(uniform(r * workgroups / left), most);
+            if (p < 2) continue;
+            const int cost = r * (uniform(steps / p) + kEndSteps) + uniform(left * p / 10) + kJoinSteps;
+            if (cost < least) { least = cost; parts = p; }
+        }
+        if (parts == 1) left = 0;
         whole = tiles - left;
     }
     __device__ __forceinline__ void place(int t, GemmItem& it) const {
@@ -83,8 +91,8 @@ struct GemmGrid {
             if (round < rounds - 1 || left == 0) return false;
             round = rounds;                          // no whole tile in the last round
         }
-        const int u = x * side + i;
-        if (left == 0 || round > rounds || u >= left * parts) return false;
+        const int u = (round - rounds) * workgroups + x * side + i;
+        if (u >= left * parts) return false;
         const int part = u / left, steps = (depth + kStepK - 1) / kStepK;
         place(whole + u - part * left, it);
         const int s0 = (int)((long long)steps * part / parts), s1 = (int)((long long)steps * (part + 1) / parts);
@@ -460,15 +468,17 @@ struct Gemm {
                     const i32x4 v = *reinterpret_cast<const WLB_LDS i32x4*>((uintptr_t)(mine + n * ROWB + ((c ^ (n & (CH - 1))) * 16)));
                     put(wn * (S::BN * 16) + j0 * 16 + n, wm * (S::BM * 16) + i0 * 16 + c * 16 / Bytes, v);
                 }
+                __builtin_amdgcn_sched_barrier(0);
                 wait_lds();
                 __builtin_amdgcn_wave_barrier();
             }
     }
 
-    // the partial sums of a divided tile: [TN][256] floats, of which `rows` are read
+    // The partial sums of a divided tile: [TN][256] floats, of which `rows` are read (wide tiles write them all: comparisons in front of 64 stores made the
+    // compiler keep registers in memory).
     __device__ __forceinline__ void part_out(uint32_t room, float* to, int rows) {
         rows_out<4>(room, [&](int i, int j, int r) __attribute__((always_inline)) { return sum(i, j, r); },
-                    [&](int n, int m, const i32x4& v) __attribute__((always_inline)) { if (n < rows) *reinterpret_cast<i32x4*>(to + n * S::TM + m) = v; });
+                    [&](int n, int m, const i32x4& v) __attribute__((always_inline)) { if (S::RING || n < rows) *reinterpret_cast<i32x4*>(to + n * S::TM + m) = v; });
     }
 };
 

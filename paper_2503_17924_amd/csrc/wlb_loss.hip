@@ -130,10 +130,9 @@ __global__ void __launch_bounds__(kRowsThreads) loss_rows_kernel(RowsArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------
-// Products and their work lists.  A wide tile is divided along k (GemmGrid) only into parts of kWideParts steps and more: its partial sums cost a write
-// and a read of 256 KiB and a launch (20 us in all, what 14 steps take; parts of 8 and more steps from 24 on: 4085 slots, 50001 words, hidden 1544, 25 steps, 615 us, undivided 601).  Narrow ones, which few slots leave to a few workgroups, from kNarrowParts on for dX,
-// else never.
-constexpr int kWideParts = 16, kNarrowParts = 4, kNever = 1 << 30;
+// Products and their work lists.  A wide tile is divided along k (GemmGrid) into parts of kWideParts steps and more, in up to kWideRounds rounds; narrow ones, which
+// few slots leave to a few workgroups, into parts of kNarrowParts and more for dX, else never.
+constexpr int kWideParts = 8, kWideRounds = 2, kNarrowParts = 4, kNever = 1 << 30;
 
 struct Work : GemmGrid {
     const __bf16 *p_at, *q_at;
@@ -145,7 +144,8 @@ struct Work : GemmGrid {
     template <class S>
     static __device__ __forceinline__ Work make(const __bf16* p, long long ldp, int pm, const __bf16* q, long long ldq, int qn, const int32_t* list, int depth,
                                                 int workgroups, int narrow_parts) {
-        Work w(GemmGrid((pm + S::TM - 1) / S::TM, (qn + S::TN - 1) / S::TN, depth, workgroups, S::RING ? kWideParts : narrow_parts));
+        Work w(GemmGrid((pm + S::TM - 1) / S::TM, (qn + S::TN - 1) / S::TN, depth, workgroups, S::RING ? kWideParts : narrow_parts,
+                        S::RING ? kWideRounds : 1));
         w.p_at = p; w.q_at = q; w.ldp = ldp; w.ldq = ldq; w.pm = pm; w.qn = qn; w.list = list;
         w.tile_m = S::TM; w.tile_n = S::TN; w.p_down = S::MP; w.q_down = S::MQ;
         return w;
@@ -667,8 +667,8 @@ static LossLayout loss_layout(const wlb_vocab_desc& d) {
     L.off_target = take(4 * n_q);
     L.off_row_lse = take(4 * n_q);
     L.off_row_weight = take(4 * n_q);
-    // a divided tile's parts are no more than the workgroups of the launch
-    L.off_parts = take(sizeof(float) * kWordTile * (size_t)L.tile * wide_workgroups());
+    // parts of divided tiles
+    L.off_parts = take(sizeof(float) * kWordTile * (size_t)L.tile * wide_workgroups() * (L.tile < 256 ? 1 : kWideRounds));
     const size_t common = at;
     L.off_part = take(sizeof(float2) * (size_t)L.word_tiles * L.pitch_rows);
     L.off_target_logit = take(4 * n_q);
@@ -719,12 +719,13 @@ static void launch_rows(const RowsArgs& a, hipStream_t stream) {
     }
 }
 
-// Wide tiles: one workgroup to a compute unit, and a join of the divided tiles (at most half as many as there are workgroups) where `depth` is long enough.
+// Wide tiles: one workgroup to a compute unit, and a join of the divided tiles where `depth` is long enough (half as many as there are workgroups at most, in one
+// round; two thirds, in two: two rounds of halves save nothing).
 template <class K, class J, class A>
 static void launch_wide(K kernel, J join, A& a, int depth, hipStream_t stream) {
     a.workgroups = wide_workgroups();
     kernel<<<a.workgroups, 256, 0, stream>>>(a);
-    if ((depth + kStepK - 1) / kStepK >= 2 * kWideParts) join<<<a.workgroups / 2 * 256 / 4, 256, 0, stream>>>(a);
+    if (depth > (2 * kWideParts - 1) * kStepK) join<<<a.workgroups * 2 / 3 * 256 / 4, 256, 0, stream>>>(a);
 }
 
 // Narrow tiles, one to a workgroup.
@@ -825,7 +826,7 @@ extern "C" wlb_status wlb_loss_bwd(const wlb_vocab_desc* desc, const void* x, co
         else launch_wide(loss_d_kernel<Wide<false, false>>, loss_d_parts_kernel<Wide<false, false>>, a, d.hidden, stream);
         // tiles of 128 x 128 where wide ones neither fill the launch nor have rows enough to be divided, and where there is but one step, in front of
         // and behind which nothing runs beside a wide tile (33 slots, 65536 words, hidden 2048: 66 us, wide 71; 128 slots: 84 and 73)
-        if (d.n_q > kStepK && ((long long)word_tiles * column_tiles >= wide_workgroups() || d.n_q >= 2 * kWideParts * kStepK))
+        if (d.n_q > kStepK && ((long long)word_tiles * column_tiles >= wide_workgroups() || d.n_q > (2 * kWideParts - 1) * kStepK))
             launch_wide(loss_dtable_kernel<Wide<true, true>>, loss_dtable_parts_kernel<Wide<true, true>>, a, d.n_q, stream);
         else launch_narrow(loss_dtable_kernel<Half<true, true>>, a, (long long)((a.piece_n + 127) / 128) * ((d.hidden + 127) / 128), stream);
         if (L.tile == 32) launch_divided(loss_dx_kernel<Slots32<true, false>>, loss_dx_parts_kernel<Slots32<true, false>>, a, 32, column_tiles, stream);
