@@ -18,7 +18,11 @@ global batch since the packers place different token counts per batch (left-over
 documents move between batches), and the documents still held back when the stream ends,
 and the a (picoseconds per token^2) that a least-squares fit of the measured latencies gives.
 
-Usage (on the GPU):  python -m paper_2503_17924_amd.packing_report [--iterations 6]
+With --vocab N the part of the linear work that this library has, the two ends of the model (lookup of the micro-batch's tokens, loss over N
+words, the gradients of both), is measured on every micro-batch too and stands in the step in addition to b * tokens, which then models the
+layers between; its own linear cost in picoseconds per token is fitted and printed.
+
+Usage (on the GPU):  python -m paper_2503_17924_amd.packing_report [--iterations 6] [--vocab 32768 [--hidden 1024]]
 """
 from __future__ import annotations
 
@@ -49,10 +53,35 @@ def arrival_windows(doc_len, window: int):
     return seqs          # the unfinished tail is left out
 
 
+def time_vocabulary(torch, B, docs, vocab, hidden, reps=2, seed=0):
+    """Median milliseconds of lookup, loss, its gradients and the lookup's, added to the table's, for one packed micro-batch (CP = 1)."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    cu = np.concatenate([[0], np.cumsum(docs)]).astype(np.int32)
+    t = int(cu[-1])
+    table = (torch.randn((vocab, hidden), device="cuda", generator=g) * (2 / hidden ** 0.5)).to(torch.bfloat16)
+    tokens = torch.randint(0, vocab, (t,), device="cuda", generator=g, dtype=torch.int32)
+    ends = B.Vocabulary(np.arange(t, dtype=np.int32), cu, vocab, hidden, embed_scale=float(hidden) ** 0.5)
+    d_loss = torch.full((t,), 1.0 / t, device="cuda")
+    ts = []
+    for i in range(reps + 1):
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        x = ends.embed(tokens, table)
+        _, lse = ends.loss(x, table, tokens)
+        dx, dtable = ends.loss_backward(x, table, tokens, lse, d_loss)
+        ends.embed_backward(tokens, dx, dtable, accumulate=True)
+        e1.record()
+        torch.cuda.synchronize()
+        ts.append(e0.elapsed_time(e1))
+    return float(np.median(ts[1:]))          # the first pass allocates
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--iterations", type=int, default=6, help="global batches to measure")
     ap.add_argument("--reps", type=int, default=2)
+    ap.add_argument("--vocab", type=int, default=0, help="words: measure the lookup and the loss over them as well")
+    ap.add_argument("--hidden", type=int, default=0, help="columns of the table (default: query heads * head dimension)")
     args = ap.parse_args()
     import torch
     sys.path.insert(0, os.path.dirname(HERE))
@@ -77,6 +106,18 @@ def main():
             t = int(cu[-1])
             cache[key] = PK.time_rank(torch, B, np.arange(t, dtype=np.int32), cu, t, hq, hkv, d, reps=args.reps)
         return cache[key]
+
+    vocab_cache = {}
+    hidden = args.hidden or hq * d
+
+    def vocabulary_ms(docs):
+        """Measured milliseconds of lookup, loss and their gradients for one packed micro-batch; 0 without --vocab."""
+        if not args.vocab:
+            return 0.0
+        key = tuple(docs)
+        if key not in vocab_cache:
+            vocab_cache[key] = time_vocabulary(torch, B, docs, args.vocab, hidden, reps=args.reps)
+        return vocab_cache[key]
 
     def fixed(_state, it, cur):
         return [seqs[it * n_mb + j] for j in range(n_mb)]
@@ -105,7 +146,7 @@ def main():
                 continue          # the queues are still filling: not every micro-batch has work yet
             model = [sum(COST_A * x * x + COST_B * x for x in m) for m in mbs]
             att = [attention_ms(m) for m in mbs]
-            step = [a_ms + COST_B * sum(m) * 1e-9 for a_ms, m in zip(att, mbs)]
+            step = [a_ms + COST_B * sum(m) * 1e-9 + vocabulary_ms(m) for a_ms, m in zip(att, mbs)]
             rows.append((imb(model), imb(att), imb(step), max(att), max(step), float(sum(sum(m) for m in mbs))))
             for a_ms, m in zip(att, mbs):
                 fit_x.append(float(sum(x * x for x in m)))
@@ -118,6 +159,11 @@ def main():
     a_fit = float((x * y).sum() / (x * x).sum()) * 1e9          # ms per token^2 -> ps per token^2
     print(f"least-squares fit of measured attention latency to a*sum(d^2): a = {a_fit:.2f} ps per token^2 "
           f"(the packers used a = {COST_A})")
+    if args.vocab:
+        x, y = np.array([sum(m) for m in vocab_cache], dtype=np.float64), np.array(list(vocab_cache.values()))
+        off = np.abs(y - x * (x * y).sum() / (x * x).sum()) / y
+        print(f"lookup, loss and gradients, {args.vocab} words, hidden {hidden}: {(x * y).sum() / (x * x).sum() * 1e9:.0f} ps per token "
+              f"(least squares; worst of {len(y)} micro-batches {off.max() * 100:.1f} % off), {100 * (x * y).sum() / (x * x).sum() * 1e9 / COST_B:.1f} % of the b that the packers used")
 
 
 if __name__ == "__main__":

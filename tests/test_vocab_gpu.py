@@ -142,9 +142,11 @@ def test_lookup_gradient_of_many_slots(docs, vocab, hidden):
     e.check_embed_bwd()
 
 
-@pytest.mark.parametrize("docs,cp,rank,vocab,hidden", [([16700], 1, 0, 33000, 64), ([2600, 400], 1, 0, 16400, 776), ([5000], 1, 0, 520, 2056)])
+@pytest.mark.parametrize("docs,cp,rank,vocab,hidden", [([16700], 1, 0, 33000, 64), ([2600, 400], 1, 0, 16400, 776), ([5000], 1, 0, 520, 2056),
+                                                       ([4900], 1, 0, 13000, 2048), ([16, 60], 1, 0, 40000, 72)])
 def test_loss_in_pieces_and_wide_tiles(docs, cp, rank, vocab, hidden):
-    """Three pieces of the vocabulary; more tiles than compute units; a long sum along few words."""
+    """Three pieces of the vocabulary; more tiles than compute units; a long sum along few words; tiles divided so that
+    their parts take two rounds; few slots and many words."""
     Ends(4, docs, cp, rank, vocab, hidden).check_loss()
 
 
@@ -279,6 +281,25 @@ def test_captured_into_a_graph_and_replayed():
         for a, b in zip(kept, eager):
             bits = torch.int32 if a.dtype == torch.float32 else torch.int16        # slots whose d_loss is no number have targets now
             assert torch.equal(a.view(bits), b.view(bits)), f"replay {k}"
+
+
+def test_memory_of_other_shapes_is_refused():
+    import torch
+    e = Ends(13, [40], 1, 0, 100, 64)
+    ends = B.Vocabulary(e.q_idx, e.cu, e.vocab, e.hidden)
+    loss, lse = ends.loss(e.x, e.table, e.tokens)
+    for call, error in ((lambda: ends.embed(e.tokens, e.table[:50]), ValueError), (lambda: ends.embed(e.tokens.long(), e.table), TypeError),
+                        (lambda: ends.embed(e.tokens, e.table.t()), TypeError), (lambda: ends.embed(e.tokens.cpu(), e.table), TypeError),
+                        (lambda: ends.loss(e.x[:-1], e.table, e.tokens), ValueError), (lambda: ends.loss(e.x.float(), e.table, e.tokens), TypeError),
+                        (lambda: ends.loss_backward(e.x, e.table, e.tokens, lse.double(), e.d_loss), TypeError),
+                        (lambda: ends.loss_backward(e.x, e.table, e.tokens, lse, e.d_loss[None]), ValueError),
+                        (lambda: ends.embed_backward(e.tokens, e.dx, accumulate=True), ValueError),
+                        (lambda: ends.embed(e.tokens, torch.empty(e.vocab * e.hidden + 1, dtype=torch.bfloat16, device=DEV)[1:].view(e.vocab, e.hidden)), B.WlbError),
+                        (lambda: B.wlb_loss_fwd(e.desc, e.x, e.table, e.tokens, e.q_dev, e.cu_dev, loss, lse, e.rooms[1].t[:-1]), B.WlbError)):
+        with pytest.raises(error):
+            call()
+    with pytest.raises(B.WlbError):
+        B.Vocabulary(e.q_idx, e.cu, 100, 60).embed(e.tokens, torch.empty(100, 60, dtype=torch.bfloat16, device=DEV))
 
 
 def test_on_another_stream():
