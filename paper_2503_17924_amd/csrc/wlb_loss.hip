@@ -388,15 +388,17 @@ __global__ void __launch_bounds__(256) loss_join_kernel(const float2* part, cons
 }
 
 // ------------------------------------------------------------------------------------------
-// Backward.  The labelled rows of x one behind the other, and zeros in dx of the other slots.
+// Backward.  The labelled rows of x one behind the other (and once more, for D's second set of rows), and zeros in dx of the other slots.
 __global__ void __launch_bounds__(256) loss_gather_kernel(const uint4* x, uint4* rows_x, uint4* dx, const int32_t* rows, const int32_t* slot_target,
-                                                          const int32_t* count, int n_q, int chunks) {
+                                                          const int32_t* count, int n_q, int chunks, int twice) {
     const int i = (int)blockIdx.x * 4 + ((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (i >= n_q) return;
-    const bool row = i < *count, none = slot_target[i] < 0;
+    const int n = *count;
+    const bool row = i < n, none = slot_target[i] < 0;
     const size_t from = row ? (size_t)rows[i] * chunks : 0;
     for (int c = lane; c < chunks; c += 64) {
         if (row) rows_x[(size_t)i * chunks + c] = x[from + c];
+        if (row && twice) rows_x[(size_t)(n + i) * chunks + c] = x[from + c];
         if (none) dx[(size_t)i * chunks + c] = uint4{0, 0, 0, 0};
     }
 }
@@ -410,9 +412,11 @@ struct GradArgs {
     float *parts;                    // divided tiles
     const int32_t *rows, *target, *count;
     const float *row_lse, *row_weight, *factor;
+    float *target_rest;              // [labelled]: what bf16 leaves out of D at the row's target
     int vocab, hidden, n_q, pitch, workgroups;
     int piece0, piece_n;             // words of the piece
     int add, final;                  // dX: there are earlier pieces; this piece is the last
+    int twice;                       // D has a second set of rows, with what bf16 leaves out of the first
     float c2;
 };
 
@@ -479,7 +483,20 @@ struct DDone {
                             l = here ? g.sum(i, j, r) : l;
                             mine |= here;
                         }
-                    if (mine) set(t + (g.lane / 16) * 4, weight[j] * (share(l, j) - 1.f));
+                    if (!mine) return;
+                    const float d = weight[j] * (share(l, j) - 1.f);
+                    set(t + (g.lane / 16) * 4, d);
+                    if (!S::RING) a.target_rest[n0 + g.wn * (S::BN * 16) + j * 16 + g.lane % 16] = d - (float)(__bf16)d;
+                });
+            if (S::RING || !a.twice) return;
+            g.template rows_out<2>(
+                room,
+                [&](int i, int j, int r) __attribute__((always_inline)) {
+                    const float p = share(g.sum(i, j, r), j), d = weight[j] * (target[j] == i * 16 + r ? p - 1.f : p);
+                    return edge && first + i * 16 + r >= a.piece_n ? 0.f : d - (float)(__bf16)d;
+                },
+                [&](int n, int m, const i32x4& v) __attribute__((always_inline)) {
+                    if (n0 + n < w.qn) *reinterpret_cast<i32x4*>(a.d + (size_t)(w.qn + n0 + n) * a.pitch + m0 + m) = v;
                 });
         };
         if (m0 + S::TM > a.piece_n) out(std::true_type{});
@@ -516,7 +533,7 @@ __global__ void __launch_bounds__(256) loss_d_parts_kernel(GradArgs a) {
 // dE of the piece: D^T X, both operands with the sum's index (the row) outermost.
 template <class S>
 __device__ __forceinline__ Work dtable_work(const GradArgs& a) {
-    return Work::make<S>(a.rows_x, a.hidden, a.hidden, a.d, a.pitch, a.piece_n, nullptr, ld_const(a.count), a.workgroups, kNever);
+    return Work::make<S>(a.rows_x, a.hidden, a.hidden, a.d, a.pitch, a.piece_n, nullptr, ld_const(a.count) * (a.twice ? 2 : 1), a.workgroups, kNever);
 }
 
 struct NothingAhead {
@@ -570,10 +587,19 @@ __device__ __forceinline__ Work dx_work(const GradArgs& a) {
     return Work::make<S>(a.table + (size_t)a.piece0 * a.hidden, a.hidden, a.hidden, a.d, a.pitch, ld_const(a.count), nullptr, a.piece_n, a.workgroups, kNarrowParts);
 }
 
+// Rest: with what bf16 left out of D at the row's target, the largest of its entries: of many rows these roundings average out, in
+// few they show (one row: up to 2^-8 of all its gradient).
+template <bool Rest>
 __device__ __forceinline__ void put_dx(const GradArgs& a, float factor, int n_rows, int row, int col, f32x4 v) {
     if (row >= n_rows || col >= a.hidden) return;
     f32x4* sum = reinterpret_cast<f32x4*>(a.dx_sum + (size_t)row * a.hidden + col);
     if (a.add) v += *sum;
+    if (Rest && a.final) {
+        const bf16x4 e = *reinterpret_cast<const bf16x4*>(a.table + (size_t)a.target[row] * a.hidden + col);
+        const float rest = a.target_rest[row];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] += rest * (float)e[k];
+    }
     if (a.final) *reinterpret_cast<bf16x4*>(a.dx + (size_t)a.rows[row] * a.hidden + col) = pack4(factor * v[0], factor * v[1], factor * v[2], factor * v[3]);
     else *sum = v;
 }
@@ -591,7 +617,7 @@ struct DxDone : NothingAhead {
         }
         const int m0 = it.tm * S::TM, n0 = it.tn * S::TN;
         g.template rows_out<4>(room, [&](int i, int j, int r) __attribute__((always_inline)) { return g.sum(i, j, r); },
-                               [&](int n, int m, const i32x4& v) __attribute__((always_inline)) { put_dx(a, factor, w.qn, n0 + n, m0 + m, __builtin_bit_cast(f32x4, v)); });
+                               [&](int n, int m, const i32x4& v) __attribute__((always_inline)) { put_dx<!S::RING>(a, factor, w.qn, n0 + n, m0 + m, __builtin_bit_cast(f32x4, v)); });
     }
 };
 
@@ -608,7 +634,7 @@ __global__ void __launch_bounds__(256) loss_dx_parts_kernel(GradArgs a) {
     const Work w = dx_work<S>(a);
     const float factor = *a.factor;
     join_parts<S>(w, a.parts, [&](int tm, int tn, int n, int m, const f32x4& v) __attribute__((always_inline)) {
-        put_dx(a, factor, w.qn, tn * S::TN + n, tm * S::TM + m, v);
+        put_dx<!S::RING>(a, factor, w.qn, tn * S::TN + n, tm * S::TM + m, v);
     });
 }
 
@@ -637,10 +663,10 @@ static unsigned tile_grid(long long tiles) { return (unsigned)((tiles + kLists -
 static int wide_workgroups() { return std::max(kLists, compute_units() / kLists * kLists); }
 
 struct LossLayout {
-    size_t off_count, off_factor, off_slot_target, off_block_count, off_block_max, off_rows, off_target, off_row_lse, off_row_weight, off_parts;
+    size_t off_count, off_factor, off_slot_target, off_block_count, off_block_max, off_rows, off_target, off_row_lse, off_row_weight, off_target_rest, off_parts;
     size_t off_part, off_target_logit, fwd_bytes;                 // forward
     size_t off_rows_x, off_d, off_dx_sum, bwd_bytes;              // backward
-    int blocks, tile, word_tile, word_tiles, pitch_rows, piece, pieces;
+    int blocks, tile, word_tile, word_tiles, pitch_rows, piece, pieces, twice;
 };
 
 static LossLayout loss_layout(const wlb_vocab_desc& d) {
@@ -667,6 +693,7 @@ static LossLayout loss_layout(const wlb_vocab_desc& d) {
     L.off_target = take(4 * n_q);
     L.off_row_lse = take(4 * n_q);
     L.off_row_weight = take(4 * n_q);
+    L.off_target_rest = take(4 * n_q);
     // parts of divided tiles
     L.off_parts = take(sizeof(float) * kWordTile * (size_t)L.tile * wide_workgroups() * (L.tile < 256 ? 1 : kWideRounds));
     const size_t common = at;
@@ -674,8 +701,10 @@ static LossLayout loss_layout(const wlb_vocab_desc& d) {
     L.off_target_logit = take(4 * n_q);
     L.fwd_bytes = at;
     at = common;
-    L.off_rows_x = take(2 * n_q * h);
-    L.off_d = take(2 * n_q * (size_t)L.piece);
+    // up to 32 slots fill half of a step of dE's sum: D's rows have room for what bf16 leaves out of them, and dE is exact but for its own rounding
+    L.twice = 2 * n_q <= (size_t)kStepK;
+    L.off_rows_x = take(2 * n_q * h * (L.twice ? 2 : 1));
+    L.off_d = take(2 * n_q * (size_t)L.piece * (L.twice ? 2 : 1));
     L.off_dx_sum = take(L.pieces > 1 ? 4 * n_q * h : 0);
     L.bwd_bytes = at;
     return L;
@@ -809,8 +838,9 @@ extern "C" wlb_status wlb_loss_bwd(const wlb_vocab_desc* desc, const void* x, co
     a.table = (const __bf16*)table; a.rows_x = (__bf16*)(ws + L.off_rows_x); a.d = (__bf16*)(ws + L.off_d);
     a.dx = (__bf16*)dx; a.dtable = (__bf16*)dtable; a.dx_sum = (float*)(ws + L.off_dx_sum);
     a.rows = r.rows; a.target = r.target; a.count = r.count; a.row_lse = r.row_lse; a.row_weight = r.row_weight; a.factor = r.factor;
+    a.target_rest = (float*)(ws + L.off_target_rest); a.twice = L.twice;
     a.vocab = d.vocab; a.hidden = d.hidden; a.n_q = d.n_q; a.pitch = L.piece; a.c2 = d.scale * kLog2e;
-    loss_gather_kernel<<<(d.n_q + 3) / 4, 256, 0, stream>>>((const uint4*)x, (uint4*)a.rows_x, (uint4*)dx, a.rows, r.slot_target, a.count, d.n_q, d.hidden / 8);
+    loss_gather_kernel<<<(d.n_q + 3) / 4, 256, 0, stream>>>((const uint4*)x, (uint4*)a.rows_x, (uint4*)dx, a.rows, r.slot_target, a.count, d.n_q, d.hidden / 8, L.twice);
     a.parts = (float*)(ws + L.off_parts);
     const bool low = L.word_tile < kWordTile;
     for (int p = 0; p < L.pieces; ++p) {

@@ -72,7 +72,8 @@ def loss(x, table, target, scale):
 
 
 def loss_bwd(x, table, target, scale, d_loss):
-    """-> (dx, dtable, bounds of both)"""
+    """-> (dx, dtable, bounds of both).  D is rounded to bf16 once.  Up to 128 slots dX has what the rounding leaves out at the targets, and up to 32 dE has
+    what it leaves out everywhere, itself rounded to bf16: u * u of the value."""
     n, h = x.shape
     f64 = dict(dtype=torch.float64, device=x.device)
     dx, dtable = torch.zeros(n, h, **f64), torch.zeros(table.shape[0], h, **f64)
@@ -89,12 +90,13 @@ def loss_bwd(x, table, target, scale, d_loss):
     hot = torch.zeros_like(p).scatter_(1, t[:, None], 1.0)
     d = g[:, None] * scale * (p - hot)
     # the exponential's error and the lse's, then 4 float roundings, then bf16
-    d_off = (g.abs() * scale)[:, None] * (p * (2 * off)[:, None] + 4 * E * (p + hot) + 2 * TINY) + U * d.abs() * (1 + 2 * off)[:, None]
+    d_off = (g.abs() * scale)[:, None] * (p * (2 * off)[:, None] + 4 * E * (p + hot) + 2 * TINY)
+    size = d.abs() * (1 + 2 * off)[:, None]
     dx[has] = d @ es
-    sums = d_off @ es.abs() + (table.shape[0] + 64) * E * (d.abs() @ es.abs())
+    sums = (d_off + U * size * (1 - hot if n <= 128 else 1)) @ es.abs() + (table.shape[0] + 64) * E * (d.abs() @ es.abs())
     dx_off[has] = sums + U * (dx[has].abs() + sums)
     dtable = d.T @ xs
-    sums = d_off.T @ xs.abs() + (len(t) + 64) * E * (d.abs().T @ xs.abs())
+    sums = (d_off + (U * U if n <= 32 else U) * size).T @ xs.abs() + (len(t) + 64) * E * (d.abs().T @ xs.abs())
     dt_off = sums + U * (dtable.abs() + sums)
     return dx, dtable, dx_off, dt_off
 
