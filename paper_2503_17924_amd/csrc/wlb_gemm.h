@@ -204,6 +204,7 @@ struct Fragments {
 
 // Work is a GemmGrid with, for an item, operands p(item) and q(item) and leading dimensions ldp, ldq.  done(gemm, item, ahead, lds) takes the sums of an
 // item; lds: 32 KiB, 8 of them each wavefront's own; ahead: what done.load(gemm, item) returned in front of the item's steps (loads that would hold up its end).
+// It returns a number of vector memory operations that each wavefront has certainly issued: the next item's first step need not wait for those.
 template <class S>
 struct Gemm {
     f32x4 acc[S::BM][S::BN];    // register r of lane l: m = 16 i + (l/16)*4 + r, n = 16 j + l%16 of the wavefront's part
@@ -350,13 +351,14 @@ struct Gemm {
         for (int r = 0; r < RQ; ++r) fq.read(r, 0, b[0]);
         const f32x4 zeros = {0.f, 0.f, 0.f, 0.f};
         int p_slot = 0, q_slot = 1;             // of this step's tiles
+        int stores = 0;
         for (int round = 1;; ++round) {
             const int steps = steps_of(it, 2);
             const bool more = work.item((int)blockIdx.x, round, next);
             const auto ahead = done.load(*this, it);
             GemmOperand next_p = {}, next_q = {};
             if (more) { next_p = work.p(next); next_q = work.q(next); }
-            auto step = [&](int s, auto fresh) __attribute__((always_inline)) {       // fresh: the sums start here
+            auto step = [&](int s, auto fresh) __attribute__((always_inline)) {       // fresh: the sums start here, behind the last item's stores
                 if (s + 2 == steps) {
                     if (more) cp.tile(next_p);
                     cp.first(next.depth, more);
@@ -370,7 +372,8 @@ struct Gemm {
                     if (kk == 1) {
                         // the step's last operands are in registers and the next step's tiles in LDS, for every wavefront
                         wait_lds();
-                        wait_vmem_le<NP>();
+                        if (fresh && stores >= 32) wait_vmem_le<NP + 32>();
+                        else wait_vmem_le<NP>();
                         __syncthreads();
                         if (s + 2 == steps) {
                             if (more) cq.tile(next_q);
@@ -404,7 +407,7 @@ struct Gemm {
             for (int s = 1; s < steps; ++s) step(s, std::false_type{});
             // the next P goes to the slot used here: each wavefront's copies to the 8 KiB that are its own
             sums_ready();
-            done(*this, it, ahead, lds + (p_slot == 0 ? 4 : p_slot - 1) * SLOT);
+            stores = done(*this, it, ahead, lds + (p_slot == 0 ? 4 : p_slot - 1) * SLOT);
             wait_lds();
             if (!more) break;
             it = next;
@@ -460,17 +463,15 @@ struct Gemm {
                             *reinterpret_cast<WLB_LDS __bf16*>((uintptr_t)(mine + row * ROWB + (((m * 2 / 16) ^ (row & (CH - 1))) * 16) + m * 2 % 16)) = (__bf16)v;
                         });
                 }
-                wait_lds();
-                __builtin_amdgcn_wave_barrier();
+                asm volatile("" ::: "memory");      // LDS takes a wavefront's accesses in their order
 #pragma unroll
                 for (int t = 0; t < 16 * H / RPI; ++t) {
                     const int n = t * RPI + lane / CH, c = lane % CH;
                     const i32x4 v = *reinterpret_cast<const WLB_LDS i32x4*>((uintptr_t)(mine + n * ROWB + ((c ^ (n & (CH - 1))) * 16)));
                     put(wn * (S::BN * 16) + j0 * 16 + n, wm * (S::BM * 16) + i0 * 16 + c * 16 / Bytes, v);
                 }
+                asm volatile("" ::: "memory");
                 __builtin_amdgcn_sched_barrier(0);
-                wait_lds();
-                __builtin_amdgcn_wave_barrier();
             }
     }
 

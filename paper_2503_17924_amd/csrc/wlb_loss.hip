@@ -216,12 +216,22 @@ __device__ __forceinline__ Work stats_work(const StatsArgs& a) {
     return Work::make<S>(a.table, a.hidden, a.vocab, a.x, a.hidden, n_rows, a.rows, a.hidden, a.workgroups, kNever);
 }
 
+// exchange a value with the lane 16 away, inside a half of the wavefront
+__device__ __forceinline__ float xrow(float x) {
+    const int xi = __builtin_bit_cast(int, x);
+    const auto r = __builtin_amdgcn_permlane16_swap(xi, xi, false, false);
+    return __builtin_bit_cast(float, (int)((threadIdx.x & 16) ? r[0] : r[1]));
+}
+
 // What belongs to a wavefront's rows n is loaded once for every row, 64 to a register, and fetched from the lane that holds it.
 template <class S> constexpr int row_regs() { return (S::BN * 16 + 63) / 64; }
 template <class S>
 __device__ __forceinline__ int row_held(const Gemm<S>& g, const GemmItem& it, int k) { return it.tn * S::TN + g.wn * (S::BN * 16) + k * 64 + g.lane % (S::BN * 16); }
 template <class T, int N>
 __device__ __forceinline__ T of_row(const T (&regs)[N], int j, int lane) { return __shfl(regs[j / 4], (j % 4) * 16 + lane % 16); }
+
+// Stores of a wavefront's part in rows_out<Bytes>, 1 KiB each, where no row or column lies past the end.
+template <class S, int Bytes> constexpr int row_stores() { return S::BM * 16 * S::BN * 16 * Bytes / 1024; }
 
 template <class S>
 struct StatsDone {
@@ -238,14 +248,20 @@ struct StatsDone {
         }
         return h;
     }
-    __device__ __forceinline__ void operator()(Gemm<S>& g, const GemmItem& it, const Ahead& ahead, uint32_t room) const {
+    __device__ __forceinline__ int operator()(Gemm<S>& g, const GemmItem& it, const Ahead& ahead, uint32_t room) const {
         if (it.part >= 0) {
             g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN), w.qn - it.tn * S::TN);
-            return;
+            return 0;
         }
         const int m0 = it.tm * S::TM, n0 = it.tn * S::TN, n_rows = w.qn;
         const int first = m0 + g.wm * (S::BM * 16) + (g.lane / 16) * 4;       // word of register 0 of block 0
         float2* s_part = (float2*)(smem + (room - g.lds));                    // [WM][TN]
+        int target[S::BN];                                                    // register that holds the target, if this lane has it
+#pragma unroll
+        for (int j = 0; j < S::BN; ++j) {
+            const int word = of_row(ahead.target, j, g.lane);
+            target[j] = word < 0 ? -1 : word - first;
+        }
         auto block = [&](int j, auto edge) __attribute__((always_inline)) {   // edge: words of the tile lie past the end
             const int n = g.wn * (S::BN * 16) + j * 16 + g.lane % 16;
             float logit[S::BM][4];
@@ -256,14 +272,14 @@ struct StatsDone {
                     const float l = g.sum(i, j, r);
                     logit[i][r] = edge && first + i * 16 + r >= a.vocab ? -INFINITY : l;
                 }
-            const int word = of_row(ahead.target, j, g.lane), t = word < 0 ? -1 : word - first;    // register that holds the target, if this lane has it
+            const int t = target[j];
             float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
             for (int i = 0; i < S::BM; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) most[r] = fmaxf(most[r], logit[i][r]);
             float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, xrow(top));
             top = fmaxf(top, xhalf(top));
             if (__any(t >= 0 && t < S::BM * 16)) {
                 float l = 0.f;
@@ -285,7 +301,7 @@ struct StatsDone {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) sum[r] += fast_exp2(__builtin_fmaf(logit[i][r], a.c2, -from));
             float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            all += __shfl_xor(all, 16);
+            all += xrow(all);
             all += xhalf(all);
             if (g.lane < 16) s_part[g.wm * S::TN + n] = float2{ref, all};
             __builtin_amdgcn_sched_barrier(0);
@@ -311,6 +327,7 @@ struct StatsDone {
             a.part[(size_t)it.tm * a.pitch + n0 + n] = float2{ref, sum};
         }
         __syncthreads();
+        return 0;
     }
 };
 
@@ -442,10 +459,10 @@ struct DDone {
         }
         return h;
     }
-    __device__ __forceinline__ void operator()(Gemm<S>& g, const GemmItem& it, const Ahead& h, uint32_t room) const {
+    __device__ __forceinline__ int operator()(Gemm<S>& g, const GemmItem& it, const Ahead& h, uint32_t room) const {
         if (it.part >= 0) {
             g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN), w.qn - it.tn * S::TN);
-            return;
+            return 0;
         }
         const int m0 = it.tm * S::TM, n0 = it.tn * S::TN;
         const int first = m0 + g.wm * (S::BM * 16) + (g.lane / 16) * 4;     // word of register 0 of block 0, in the piece
@@ -501,6 +518,7 @@ struct DDone {
         };
         if (m0 + S::TM > a.piece_n) out(std::true_type{});
         else out(std::false_type{});
+        return n0 + S::TN <= w.qn ? row_stores<S, 2>() : 0;
     }
 };
 
@@ -548,10 +566,10 @@ struct DtableDone : NothingAhead {
     const Work& w;
     float factor;
     __device__ __forceinline__ DtableDone(const GradArgs& a_, const Work& w_) : a(a_), w(w_), factor(*a_.factor) {}
-    __device__ __forceinline__ void operator()(Gemm<S>& g, const GemmItem& it, Ahead, uint32_t room) const {
+    __device__ __forceinline__ int operator()(Gemm<S>& g, const GemmItem& it, Ahead, uint32_t room) const {
         if (it.part >= 0) {
             g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN), w.qn - it.tn * S::TN);
-            return;
+            return 0;
         }
         const int m0 = it.tm * S::TM, n0 = it.tn * S::TN;
         g.template rows_out<2>(room, [&](int i, int j, int r) __attribute__((always_inline)) { return factor * g.sum(i, j, r); },
@@ -559,6 +577,7 @@ struct DtableDone : NothingAhead {
                                    if (n0 + n < a.piece_n && m0 + m < a.hidden)
                                        *reinterpret_cast<i32x4*>(a.dtable + (size_t)(a.piece0 + n0 + n) * a.hidden + m0 + m) = v;
                                });
+        return n0 + S::TN <= a.piece_n && m0 + S::TM <= a.hidden ? row_stores<S, 2>() : 0;
     }
 };
 
@@ -610,14 +629,15 @@ struct DxDone : NothingAhead {
     const Work& w;
     float factor;
     __device__ __forceinline__ DxDone(const GradArgs& a_, const Work& w_) : a(a_), w(w_), factor(*a_.factor) {}
-    __device__ __forceinline__ void operator()(Gemm<S>& g, const GemmItem& it, Ahead, uint32_t room) const {
+    __device__ __forceinline__ int operator()(Gemm<S>& g, const GemmItem& it, Ahead, uint32_t room) const {
         if (it.part >= 0) {
             g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN), w.qn - it.tn * S::TN);
-            return;
+            return 0;
         }
         const int m0 = it.tm * S::TM, n0 = it.tn * S::TN;
         g.template rows_out<4>(room, [&](int i, int j, int r) __attribute__((always_inline)) { return g.sum(i, j, r); },
                                [&](int n, int m, const i32x4& v) __attribute__((always_inline)) { put_dx<!S::RING>(a, factor, w.qn, n0 + n, m0 + m, __builtin_bit_cast(f32x4, v)); });
+        return n0 + S::TN <= w.qn && m0 + S::TM <= a.hidden ? row_stores<S, 4>() : 0;
     }
 };
 
