@@ -26,18 +26,21 @@ __device__ __forceinline__ int swz_m(int r, int cc) { return cc ^ (((r & 3) << 2
 constexpr int kOutOfRange = (int)0xfffffff0u;      // a lane offset at which every buffer load returns 0
 constexpr uint32_t kMaxRecords = 0xffffffe0u;
 
-template <int WM_, int WN_, int BM_, int BN_, bool MP_, bool MQ_>
+template <int WM_, int WN_, int BM_, int BN_, bool MP_, bool MQ_, int KS_ = kStepK>
 struct GemmShape {
     static constexpr int WM = WM_, WN = WN_, BM = BM_, BN = BN_;         // wavefronts, and blocks of 16 of a wavefront
+    static constexpr int KS = KS_;                                       // k of a step
     static constexpr bool MP = MP_, MQ = MQ_;                            // operand kinds: m / n contiguous in memory
     static constexpr int TM = WM * BM * 16, TN = WN * BN * 16;
-    static constexpr int P_BYTES = TM * kStepK * 2, Q_BYTES = TN * kStepK * 2, STAGE = P_BYTES + Q_BYTES;
-    // Five LDS slots of one operand's tile, or two buffers of both tiles
-    static constexpr bool RING = P_BYTES == 32768 && Q_BYTES == 32768;
-    static constexpr int LDS_BYTES = RING ? 5 * P_BYTES : 2 * STAGE;
-    static constexpr int PER_CU = LDS_BYTES > 81920 ? 1 : 2;             // workgroups to a compute unit
-    static_assert(WM * WN == 4, "four wavefronts");
-    static_assert(LDS_BYTES >= 4 * 8192, "8 KiB of each wavefront's output on its way to memory");
+    static constexpr int P_BYTES = TM * KS * 2, Q_BYTES = TN * KS * 2, STAGE = P_BYTES + Q_BYTES;
+    static constexpr bool RING = TM == 256 && TN == 256;
+    // a wavefront's output on its way to memory: 32 rows of its bf16 values, or of 64 floats where sums are kept in parts
+    static constexpr int OUT_WAVE = RING || (MP && !MQ) ? 8192 : BM * 1024;
+    // five LDS slots of one operand's tile, one of them free for the output at an item's end; or two buffers of both tiles, and the output
+    static constexpr int LDS_BYTES = RING ? 5 * P_BYTES : 2 * STAGE + 4 * OUT_WAVE;
+    static constexpr int PER_CU = LDS_BYTES > 81920 || TN >= 128 && !MQ ? 1 : 2;        // workgroups to a compute unit
+    static_assert(WM * WN == 4 && (KS == kStepK || !(RING || MP || MQ)), "four wavefronts; long steps for narrow tiles of kind K");
+    static_assert(LDS_BYTES <= 163840, "LDS of a compute unit");
 };
 
 // A piece of work of a workgroup: a tile, and which part of k.
@@ -110,11 +113,19 @@ struct GemmOperand {
     const int32_t* list;        // kind K: numbers of the rows counted from `at`, or null
 };
 
+// Place of 16-byte chunk cc of row r in an LDS tile of kind K whose rows hold KS values: 16 rows x one chunk, as the operands are read, lie in 16 different
+// chunks of 256 bytes.
+template <int KS>
+__device__ __forceinline__ int swz_k(int r, int cc) {
+    static_assert(KS == 64 || KS == 256, "rows of 128 or 512 bytes");
+    return KS == 64 ? swz<8>(r, cc) : cc ^ (r & 15);
+}
+
 // Copies of one operand's tile.  T: its width (rows of kind K, columns of kind M).
-template <int T, bool M>
+template <int T, bool M, int KS>
 struct TileCopy {
-    static constexpr int N = T * kStepK * 2 / 1024 / 4;         // 1 KiB instructions per wavefront and step
-    static constexpr int CH = M ? T / 8 : 8;                    // 16-byte chunks per LDS row
+    static constexpr int N = T * KS * 2 / 1024 / 4;             // 1 KiB instructions per wavefront and step
+    static constexpr int CH = M ? T / 8 : KS / 8;               // 16-byte chunks per LDS row
     static constexpr int RPI = 64 / CH;                         // LDS rows per instruction
     static_assert(N >= 1, "tile too narrow");
     int voff[N];
@@ -124,7 +135,7 @@ struct TileCopy {
     int wave, lane, left;                                       // k that exist from this step's start on
 
     __device__ __forceinline__ int row_of(int n) const { return (wave * N + n) * RPI + lane / CH; }
-    __device__ __forceinline__ int chunk_of(int n) const { return M ? swz_m(row_of(n), lane % CH) : swz<8>(row_of(n), lane % 8); }
+    __device__ __forceinline__ int chunk_of(int n) const { return M ? swz_m(row_of(n), lane % CH) : swz_k<KS>(row_of(n), lane % CH); }
     // ld: elements between rows
     __device__ __forceinline__ void init(long long ld, int wave_, int lane_) {
         row_bytes = (uint32_t)(ld * 2);
@@ -151,14 +162,14 @@ struct TileCopy {
         left = depth;
     }
     __device__ __forceinline__ void next() {
-        const uint64_t a = (((uint64_t)(uint32_t)rs.r[1] << 32) | (uint32_t)rs.r[0]) + (uint64_t)(M ? kStepK * row_bytes : kStepK * 2u);
+        const uint64_t a = (((uint64_t)(uint32_t)rs.r[1] << 32) | (uint32_t)rs.r[0]) + (uint64_t)(M ? KS * row_bytes : KS * 2u);
         rs.r[0] = (int)(uint32_t)a;
         rs.r[1] = (int)(uint32_t)(a >> 32);
-        left -= kStepK;
+        left -= KS;
     }
     // in the last step of a tile: lanes whose k does not exist load zeros from here on
     __device__ __forceinline__ void cut() {
-        if (left >= kStepK) return;
+        if (left >= KS) return;
 #pragma unroll
         for (int n = 0; n < N; ++n)
             if ((M ? row_of(n) : chunk_of(n) * 8) >= left) voff[n] = kOutOfRange;
@@ -167,10 +178,10 @@ struct TileCopy {
 };
 
 // Operand fragments of a wavefront out of LDS: B blocks of 16 rows (columns).
-template <int T, int B, bool M>
+template <int T, int B, bool M, int KS>
 struct Fragments {
-    static constexpr int READS = M ? 2 * B : B;
-    uint32_t at[M ? B : 2];         // K: by 32-step, the blocks 2048 bytes apart; M: by block, the 32-steps 32 rows apart
+    static constexpr int READS = M ? 2 * B : B, KN = KS / 32;
+    uint32_t at[M ? B : KN];        // K: by 32-step, the blocks 16 rows apart; M: by block, the 32-steps 32 rows apart
 
     __device__ __forceinline__ void init(uint32_t tile, int first, int lane) {
         if (M) {
@@ -182,12 +193,12 @@ struct Fragments {
         } else {
             const int row = first * 16 + lane % 16;
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk) at[kk] = tile + row * 128 + swz<8>(row, 4 * kk + lane / 16) * 16;
+            for (int kk = 0; kk < KN; ++kk) at[kk] = tile + row * (KS * 2) + swz_k<KS>(row, 4 * kk + lane / 16) * 16;
         }
     }
     __device__ __forceinline__ void move(int bytes) {
 #pragma unroll
-        for (int i = 0; i < (M ? B : 2); ++i) at[i] += bytes;
+        for (int i = 0; i < (M ? B : KN); ++i) at[i] += bytes;
     }
     // read r of READS of 32-step kk into f
     __device__ __forceinline__ void read(int r, int kk, bf16x8 (&f)[B]) const {
@@ -197,26 +208,27 @@ struct Fragments {
 #pragma unroll
             for (int e = 0; e < 4; ++e) f[i][4 * h + e] = v[e];
         } else {
-            f[r] = *reinterpret_cast<const WLB_LDS bf16x8*>((uintptr_t)(at[kk] + r * 2048));
+            f[r] = *reinterpret_cast<const WLB_LDS bf16x8*>((uintptr_t)(at[kk] + r * (16 * KS * 2)));
         }
     }
 };
 
 // Work is a GemmGrid with, for an item, operands p(item) and q(item) and leading dimensions ldp, ldq.  done(gemm, item, ahead, lds) takes the sums of an
-// item; lds: 32 KiB, 8 of them each wavefront's own; ahead: what done.load(gemm, item) returned in front of the item's steps (loads that would hold up its end).
+// item; lds: OUT_WAVE bytes for each wavefront; ahead: what done.load(gemm, item) returned in front of the item's steps (loads that would hold up its end).
 // It returns a number of vector memory operations that each wavefront has certainly issued: the next item's first step need not wait for those.
 template <class S>
 struct Gemm {
     f32x4 acc[S::BM][S::BN];    // register r of lane l: m = 16 i + (l/16)*4 + r, n = 16 j + l%16 of the wavefront's part
     int wave, lane, wm, wn;
     uint32_t lds;
-    TileCopy<S::TM, S::MP> cp;
-    TileCopy<S::TN, S::MQ> cq;
-    Fragments<S::TM, S::BM, S::MP> fp;
-    Fragments<S::TN, S::BN, S::MQ> fq;
+    TileCopy<S::TM, S::MP, S::KS> cp;
+    TileCopy<S::TN, S::MQ, S::KS> cq;
+    Fragments<S::TM, S::BM, S::MP, S::KS> fp;
+    Fragments<S::TN, S::BN, S::MQ, S::KS> fq;
     static constexpr int NP = decltype(cp)::N, NQ = decltype(cq)::N, RP = decltype(fp)::READS, RQ = decltype(fq)::READS;
 
-    static __device__ __forceinline__ int steps_of(const GemmItem& it, int least) { return max((it.depth + kStepK - 1) / kStepK, least); }
+    // An item has two steps at least (the second may be zeros), so that the steps two ahead of its last two are the next item's first two.
+    static __device__ __forceinline__ int steps_of(const GemmItem& it) { return max((it.depth + S::KS - 1) / S::KS, 2); }
 
     __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -240,86 +252,97 @@ struct Gemm {
         else pair(work, done);
     }
 
-    // One item at a time in two LDS buffers: narrow tiles, of which two workgroups share a compute unit.
+    // Narrow tiles in two LDS buffers of both operands.  Here too copies go on from one item to the next while sums go to memory.
     template <class Work, class Done>
     __device__ __forceinline__ void pair(const Work& work, const Done& done) {
-        constexpr int BM = S::BM, BN = S::BN;
-        GemmItem it;
-        for (int round = 0; work.item((int)blockIdx.x, round, it); ++round) {
-            const int steps = steps_of(it, 1);
+        constexpr int BM = S::BM, BN = S::BN, KN = S::KS / 32;
+        GemmItem it, next = {};
+        if (!work.item((int)blockIdx.x, 0, it)) return;
+        cp.tile(work.p(it));
+        cq.tile(work.q(it));
+        fp.init(lds, wm * BM, lane);
+        fq.init(lds + S::P_BYTES, wn * BN, lane);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            if (s) { cp.next(); cq.next(); }
+            else { cp.first(it.depth, true); cq.first(it.depth, true); }
+            cp.cut();
+            cq.cut();
+#pragma unroll
+            for (int n = 0; n < NP; ++n) cp.issue(n, lds + s * S::STAGE);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) cq.issue(n, lds + s * S::STAGE + S::P_BYTES);
+        }
+        bf16x8 a[2][BM], b[2][BN];
+        wait_vmem_le<NP + NQ>();
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < RP; ++r) fp.read(r, 0, a[0]);
+#pragma unroll
+        for (int r = 0; r < RQ; ++r) fq.read(r, 0, b[0]);
+        int buffer = 0;                         // of this step
+        for (int round = 1;; ++round) {
+            const int steps = steps_of(it);
+            const bool more = work.item((int)blockIdx.x, round, next);
+            GemmOperand next_p = {}, next_q = {};
+            if (more) { next_p = work.p(next); next_q = work.q(next); }
             const auto ahead = done.load(*this, it);
             clear();
-            cp.tile(work.p(it));
-            cq.tile(work.q(it));
-            fp.init(lds, wm * BM, lane);
-            fq.init(lds + S::P_BYTES, wn * BN, lane);
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                if (s) { cp.next(); cq.next(); }
-                else { cp.first(it.depth, true); cq.first(it.depth, true); }
-                cp.cut();
-                cq.cut();
-#pragma unroll
-                for (int n = 0; n < NP; ++n) cp.issue(n, lds + s * S::STAGE);
-#pragma unroll
-                for (int n = 0; n < NQ; ++n) cq.issue(n, lds + s * S::STAGE + S::P_BYTES);
-            }
-            bf16x8 a[2][BM], b[2][BN];
-            wait_vmem_le<NP + NQ>();
-            __syncthreads();
-#pragma unroll
-            for (int r = 0; r < RP; ++r) fp.read(r, 0, a[0]);
-#pragma unroll
-            for (int r = 0; r < RQ; ++r) fq.read(r, 0, b[0]);
             for (int s = 0; s < steps; ++s) {
-                const uint32_t stage = lds + (s & 1) * S::STAGE;
+                const uint32_t stage = lds + buffer * S::STAGE;
 #pragma unroll
-                for (int kk = 0; kk < 2; ++kk) {
-                    if (kk == 1) {
+                for (int kk = 0; kk < KN; ++kk) {
+                    const int then = (kk + 1) % KN;
+                    if (then == 0) {
                         // the step's last operands are in registers and the next step's tiles in LDS, for every wavefront
                         wait_lds();
                         wait_vmem();
                         __syncthreads();
-                        cp.next();
-                        cq.next();
+                        if (s + 2 == steps) {
+                            if (more) { cp.tile(next_p); cq.tile(next_q); }
+                            cp.first(next.depth, more);
+                            cq.first(next.depth, more);
+                        } else {
+                            cp.next();
+                            cq.next();
+                        }
                         cp.cut();
                         cq.cut();
-                        const int flip = (s & 1) ? -S::STAGE : S::STAGE;
+                        const int flip = buffer ? -S::STAGE : S::STAGE;
                         fp.move(flip);
                         fq.move(flip);
+                        buffer ^= 1;
                     }
 #pragma unroll
-                    for (int x = 0; x < BM * BN || x < RP + RQ || (kk == 1 && x < NP + NQ); ++x) {
+                    for (int x = 0; x < BM * BN || x < RP + RQ || (then == 0 && x < NP + NQ); ++x) {
                         // reads of the operands of the next 32-step, copies of the step after the next, MFMAs of this one
-                        if (x < RQ) fq.read(x, kk ^ 1, b[kk ^ 1]);
-                        else if (x < RP + RQ) fp.read(x - RQ, kk ^ 1, a[kk ^ 1]);
-                        if (kk == 1) {
+                        if (x < RQ) fq.read(x, then, b[then & 1]);
+                        else if (x < RP + RQ) fp.read(x - RQ, then, a[then & 1]);
+                        if (then == 0) {
                             if (x < NP) cp.issue(x, stage);
                             else if (x < NP + NQ) cq.issue(x - NP, stage + S::P_BYTES);
                         }
                         if (x < BM * BN) {
                             const int i = x / BN, j = x % BN;
-                            acc[i][j] = mfma16(a[kk][i], b[kk][j], acc[i][j]);
+                            acc[i][j] = mfma16(a[kk & 1][i], b[kk & 1][j], acc[i][j]);
                         }
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
             }
+            done(*this, it, ahead, lds + 2 * S::STAGE);
             wait_lds();
-            wait_vmem();
-            __syncthreads();
-            done(*this, it, ahead, lds);
-            wait_lds();
-            __syncthreads();
+            if (!more) break;
+            it = next;
         }
+        wait_vmem();
     }
 
     // Wide tiles.  The operands' tiles P0 Q0 P1 Q1 .. go to five LDS slots in turn, and on without a break from one item to the next:
     // while an item's sums go to memory, the first two steps of the next are in LDS or on their way, and the slot that is left holds the output.  Copies
     // take half of the time that the vector memory path has (64 KiB of 128 a step), so they are spread over the step: four wavefronts that
     // issued all of them in one quarter of it waited for each other (10 % more time).  Step s copies P of s + 2 beside its first
-    // 32-step, into the slot that Q of s - 1 left, and behind the step's barrier Q of s + 2 into the slot of its own P.  An item has two steps
-    // at least (the second may be zeros), so that the steps two ahead of its last two are the next item's first two.
+    // 32-step, into the slot that Q of s - 1 left, and behind the step's barrier Q of s + 2 into the slot of its own P. 
     template <class Work, class Done>
     __device__ __forceinline__ void ring(const Work& work, const Done& done) {
         constexpr int BM = S::BM, BN = S::BN, SLOT = S::P_BYTES;
@@ -353,7 +376,7 @@ struct Gemm {
         int p_slot = 0, q_slot = 1;             // of this step's tiles
         int stores = 0;
         for (int round = 1;; ++round) {
-            const int steps = steps_of(it, 2);
+            const int steps = steps_of(it);
             const bool more = work.item((int)blockIdx.x, round, next);
             const auto ahead = done.load(*this, it);
             GemmOperand next_p = {}, next_q = {};
@@ -438,8 +461,8 @@ struct Gemm {
     __device__ __forceinline__ void rows_out(uint32_t room, V value, Put put, Mend mend = Mend{}) {
         constexpr int MOST = 256 / (16 * Bytes), G = S::BM < MOST ? S::BM : MOST, H = S::BN < 2 ? S::BN : 2;    // blocks of 16 m, of 16 n at a time
         constexpr int ROWB = G * 16 * Bytes, CH = ROWB / 16, RPI = 64 / CH;                      // bytes, chunks of a row; rows per pass
-        static_assert(S::BM % G == 0 && S::BN % H == 0 && ROWB <= 256 && 16 * H % RPI == 0, "8 KiB of a wavefront");
-        const uint32_t mine = room + wave * 8192;
+        static_assert(S::BM % G == 0 && S::BN % H == 0 && ROWB <= 256 && 16 * H % RPI == 0, "whole passes");
+        const uint32_t mine = room + wave * S::OUT_WAVE;
 #pragma unroll
         for (int j0 = 0; j0 < S::BN; j0 += H)
 #pragma unroll
@@ -478,6 +501,7 @@ struct Gemm {
     // The partial sums of a divided tile: [TN][256] floats, of which `rows` are read (wide tiles write them all: comparisons in front of 64 stores made the
     // compiler keep registers in memory).
     __device__ __forceinline__ void part_out(uint32_t room, float* to, int rows) {
+        static_assert(S::OUT_WAVE == 8192, "32 rows of 64 floats");
         rows_out<4>(room, [&](int i, int j, int r) __attribute__((always_inline)) { return sum(i, j, r); },
                     [&](int n, int m, const i32x4& v) __attribute__((always_inline)) { if (S::RING || n < rows) *reinterpret_cast<i32x4*>(to + n * S::TM + m) = v; });
     }

@@ -249,10 +249,11 @@ struct StatsDone {
         return h;
     }
     __device__ __forceinline__ int operator()(Gemm<S>& g, const GemmItem& it, const Ahead& ahead, uint32_t room) const {
-        if (it.part >= 0) {
-            g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN), w.qn - it.tn * S::TN);
-            return 0;
-        }
+        if constexpr (S::OUT_WAVE == 8192)          // other tiles are never divided
+            if (it.part >= 0) {
+                g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN), w.qn - it.tn * S::TN);
+                return 0;
+            }
         const int m0 = it.tm * S::TM, n0 = it.tn * S::TN, n_rows = w.qn;
         const int first = m0 + g.wm * (S::BM * 16) + (g.lane / 16) * 4;       // word of register 0 of block 0
         float2* s_part = (float2*)(smem + (room - g.lds));                    // [WM][TN]
@@ -460,10 +461,11 @@ struct DDone {
         return h;
     }
     __device__ __forceinline__ int operator()(Gemm<S>& g, const GemmItem& it, const Ahead& h, uint32_t room) const {
-        if (it.part >= 0) {
-            g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN), w.qn - it.tn * S::TN);
-            return 0;
-        }
+        if constexpr (S::OUT_WAVE == 8192)          // other tiles are never divided
+            if (it.part >= 0) {
+                g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN), w.qn - it.tn * S::TN);
+                return 0;
+            }
         const int m0 = it.tm * S::TM, n0 = it.tn * S::TN;
         const int first = m0 + g.wm * (S::BM * 16) + (g.lane / 16) * 4;     // word of register 0 of block 0, in the piece
         float lse2[S::BN], weight[S::BN];
@@ -567,10 +569,11 @@ struct DtableDone : NothingAhead {
     float factor;
     __device__ __forceinline__ DtableDone(const GradArgs& a_, const Work& w_) : a(a_), w(w_), factor(*a_.factor) {}
     __device__ __forceinline__ int operator()(Gemm<S>& g, const GemmItem& it, Ahead, uint32_t room) const {
-        if (it.part >= 0) {
-            g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN), w.qn - it.tn * S::TN);
-            return 0;
-        }
+        if constexpr (S::OUT_WAVE == 8192)          // other tiles are never divided
+            if (it.part >= 0) {
+                g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN), w.qn - it.tn * S::TN);
+                return 0;
+            }
         const int m0 = it.tm * S::TM, n0 = it.tn * S::TN;
         g.template rows_out<2>(room, [&](int i, int j, int r) __attribute__((always_inline)) { return factor * g.sum(i, j, r); },
                                [&](int n, int m, const i32x4& v) __attribute__((always_inline)) {
@@ -630,10 +633,11 @@ struct DxDone : NothingAhead {
     float factor;
     __device__ __forceinline__ DxDone(const GradArgs& a_, const Work& w_) : a(a_), w(w_), factor(*a_.factor) {}
     __device__ __forceinline__ int operator()(Gemm<S>& g, const GemmItem& it, Ahead, uint32_t room) const {
-        if (it.part >= 0) {
-            g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN), w.qn - it.tn * S::TN);
-            return 0;
-        }
+        if constexpr (S::OUT_WAVE == 8192)          // other tiles are never divided
+            if (it.part >= 0) {
+                g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN), w.qn - it.tn * S::TN);
+                return 0;
+            }
         const int m0 = it.tm * S::TM, n0 = it.tn * S::TN;
         g.template rows_out<4>(room, [&](int i, int j, int r) __attribute__((always_inline)) { return g.sum(i, j, r); },
                                [&](int n, int m, const i32x4& v) __attribute__((always_inline)) { put_dx<!S::RING>(a, factor, w.qn, n0 + n, m0 + m, __builtin_bit_cast(f32x4, v)); });
@@ -669,6 +673,9 @@ template <bool MP, bool MQ> using Slots32 = GemmShape<4, 1, 4, 2, MP, MQ>;
 using Slots128Low = GemmShape<4, 1, 2, 8, false, false>;
 using Slots64Low = GemmShape<4, 1, 2, 4, false, false>;
 using Slots32Low = GemmShape<4, 1, 2, 2, false, false>;
+// 64 words in steps of 256: the memory gives pieces of 512 bytes of a table's rows faster than pieces of 128 (a plain read 5.3 and 4.3 TB/s)
+using Slots32Long = GemmShape<4, 1, 1, 2, false, false, 256>;
+constexpr int kLongHidden = 1024;
 
 static int slot_tile(int n_q) { return n_q <= 32 ? 32 : n_q <= 64 ? 64 : n_q <= 128 ? 128 : 256; }
 
@@ -695,7 +702,9 @@ static LossLayout loss_layout(const wlb_vocab_desc& d) {
     L.blocks = (d.n_q + kRowsThreads - 1) / kRowsThreads;
     L.tile = slot_tile(d.n_q);
     // Few slots: tiles of 128 words where those of 256 are fewer than the compute units (32768 words, hidden 1024, 65 slots: statistics 19 us, with 256 33).
-    L.word_tile = L.tile < 256 && (d.vocab + kWordTile - 1) / kWordTile < compute_units() ? kWordTile / 2 : kWordTile;
+    // Up to 32 slots: of 64, where rows hold four long steps (131072 words, hidden 2048, 20 slots: 108 us, with 256 126; 50000 words, hidden 512: 16 and 11).
+    L.word_tile = L.tile == 32 && d.hidden >= kLongHidden ? kWordTile / 4
+                  : L.tile < 256 && (d.vocab + kWordTile - 1) / kWordTile < compute_units() ? kWordTile / 2 : kWordTile;
     L.word_tiles = (d.vocab + L.word_tile - 1) / L.word_tile;
     L.pitch_rows = (int)align_up(n_q, 64);
     const size_t words = align_up(v, kWordTile);
@@ -738,7 +747,7 @@ static wlb_status check_loss(const wlb_vocab_desc* desc, const char* call) {
     // rows of x are addressed with 32-bit offsets
     if ((uint64_t)desc->n_q * desc->hidden * 2 >= (1ull << 32) - (1u << 20))
         return fail(WLB_ERR_UNSUPPORTED, "%s: x of 4 GiB or more is not supported", call);
-    if ((int64_t)(desc->vocab / (kWordTile / 2) + 1) * (desc->n_q / 32 + 1) > (1 << 30))
+    if ((int64_t)(desc->vocab / (kWordTile / 4) + 1) * (desc->n_q / 32 + 1) > (1 << 30))
         return fail(WLB_ERR_UNSUPPORTED, "%s: vocab=%d words for n_q=%d slots", call, desc->vocab, desc->n_q);
     return WLB_OK;
 }
@@ -777,10 +786,10 @@ static void launch_wide(K kernel, J join, A& a, int depth, hipStream_t stream) {
     if (depth > (2 * kWideParts - 1) * kStepK) join<<<a.workgroups * 2 / 3 * 256 / 4, 256, 0, stream>>>(a);
 }
 
-// Narrow tiles, one to a workgroup.
-template <class K, class A>
+// Narrow tiles of shape S, none of them divided.
+template <class S, class K, class A>
 static void launch_narrow(K kernel, A& a, long long tiles, hipStream_t stream) {
-    a.workgroups = (int)tile_grid(tiles);
+    a.workgroups = (int)std::min((long long)tile_grid(tiles), (long long)wide_workgroups() * S::PER_CU);
     kernel<<<a.workgroups, 256, 0, stream>>>(a);
 }
 
@@ -826,9 +835,13 @@ extern "C" wlb_status wlb_loss_fwd(const wlb_vocab_desc* desc, const void* x, co
     a.vocab = d.vocab; a.hidden = d.hidden; a.pitch = L.pitch_rows; a.c2 = d.scale * kLog2e;
     a.parts = (float*)(ws + L.off_parts);
     const bool low = L.word_tile < kWordTile;
-    if (L.tile == 32) launch_narrow(low ? loss_stats_kernel<Slots32Low> : loss_stats_kernel<Slots32<false, false>>, a, L.word_tiles, stream);
-    else if (L.tile == 64) launch_narrow(low ? loss_stats_kernel<Slots64Low> : loss_stats_kernel<Slots64<false, false>>, a, L.word_tiles, stream);
-    else if (L.tile == 128) launch_narrow(low ? loss_stats_kernel<Slots128Low> : loss_stats_kernel<Slots128<false, false>>, a, L.word_tiles, stream);
+    if (L.word_tile == kWordTile / 4) launch_narrow<Slots32Long>(loss_stats_kernel<Slots32Long>, a, L.word_tiles, stream);
+    else if (L.tile == 32) low ? launch_narrow<Slots32Low>(loss_stats_kernel<Slots32Low>, a, L.word_tiles, stream)
+                           : launch_narrow<Slots32<false, false>>(loss_stats_kernel<Slots32<false, false>>, a, L.word_tiles, stream);
+    else if (L.tile == 64) low ? launch_narrow<Slots64Low>(loss_stats_kernel<Slots64Low>, a, L.word_tiles, stream)
+                           : launch_narrow<Slots64<false, false>>(loss_stats_kernel<Slots64<false, false>>, a, L.word_tiles, stream);
+    else if (L.tile == 128) low ? launch_narrow<Slots128Low>(loss_stats_kernel<Slots128Low>, a, L.word_tiles, stream)
+                           : launch_narrow<Slots128<false, false>>(loss_stats_kernel<Slots128<false, false>>, a, L.word_tiles, stream);
     else launch_wide(loss_stats_kernel<Wide<false, false>>, loss_stats_parts_kernel<Wide<false, false>>, a, d.hidden, stream);
     if (L.tile < 256) loss_join_kernel<4><<<(d.n_q + 3) / 4, 256, 0, stream>>>(a.part, a.target_logit, a.rows, a.count, loss, lse, L.word_tiles, L.pitch_rows, a.c2);
     else loss_join_kernel<32><<<(d.n_q + 31) / 32, 256, 0, stream>>>(a.part, a.target_logit, a.rows, a.count, loss, lse, L.word_tiles, L.pitch_rows, a.c2);
@@ -870,15 +883,19 @@ extern "C" wlb_status wlb_loss_bwd(const wlb_vocab_desc* desc, const void* x, co
         a.final = p == L.pieces - 1;
         const int word_tiles = (a.piece_n + kWordTile - 1) / kWordTile, column_tiles = (d.hidden + kWordTile - 1) / kWordTile;
         const int few_tiles = (a.piece_n + L.word_tile - 1) / L.word_tile;
-        if (L.tile == 32) launch_narrow(low ? loss_d_kernel<Slots32Low> : loss_d_kernel<Slots32<false, false>>, a, few_tiles, stream);
-        else if (L.tile == 64) launch_narrow(low ? loss_d_kernel<Slots64Low> : loss_d_kernel<Slots64<false, false>>, a, few_tiles, stream);
-        else if (L.tile == 128) launch_narrow(low ? loss_d_kernel<Slots128Low> : loss_d_kernel<Slots128<false, false>>, a, few_tiles, stream);
+        if (L.word_tile == kWordTile / 4) launch_narrow<Slots32Long>(loss_d_kernel<Slots32Long>, a, few_tiles, stream);
+        else if (L.tile == 32) low ? launch_narrow<Slots32Low>(loss_d_kernel<Slots32Low>, a, few_tiles, stream)
+                               : launch_narrow<Slots32<false, false>>(loss_d_kernel<Slots32<false, false>>, a, few_tiles, stream);
+        else if (L.tile == 64) low ? launch_narrow<Slots64Low>(loss_d_kernel<Slots64Low>, a, few_tiles, stream)
+                               : launch_narrow<Slots64<false, false>>(loss_d_kernel<Slots64<false, false>>, a, few_tiles, stream);
+        else if (L.tile == 128) low ? launch_narrow<Slots128Low>(loss_d_kernel<Slots128Low>, a, few_tiles, stream)
+                               : launch_narrow<Slots128<false, false>>(loss_d_kernel<Slots128<false, false>>, a, few_tiles, stream);
         else launch_wide(loss_d_kernel<Wide<false, false>>, loss_d_parts_kernel<Wide<false, false>>, a, d.hidden, stream);
         // tiles of 128 x 128 where wide ones neither fill the launch nor have rows enough to be divided, and where there is but one step, in front of
         // and behind which nothing runs beside a wide tile (33 slots, 65536 words, hidden 2048: 66 us, wide 71; 128 slots: 84 and 73)
         if (d.n_q > kStepK && ((long long)word_tiles * column_tiles >= wide_workgroups() || d.n_q > (2 * kWideParts - 1) * kStepK))
             launch_wide(loss_dtable_kernel<Wide<true, true>>, loss_dtable_parts_kernel<Wide<true, true>>, a, d.n_q, stream);
-        else launch_narrow(loss_dtable_kernel<Half<true, true>>, a, (long long)((a.piece_n + 127) / 128) * ((d.hidden + 127) / 128), stream);
+        else launch_narrow<Half<true, true>>(loss_dtable_kernel<Half<true, true>>, a, (long long)((a.piece_n + 127) / 128) * ((d.hidden + 127) / 128), stream);
         if (L.tile == 32) launch_divided(loss_dx_kernel<Slots32<true, false>>, loss_dx_parts_kernel<Slots32<true, false>>, a, 32, column_tiles, stream);
         else if (L.tile == 64) launch_divided(loss_dx_kernel<Slots64<true, false>>, loss_dx_parts_kernel<Slots64<true, false>>, a, 64, column_tiles, stream);
         else if (L.tile == 128) launch_divided(loss_dx_kernel<Slots128<true, false>>, loss_dx_parts_kernel<Slots128<true, false>>, a, 128, column_tiles, stream);

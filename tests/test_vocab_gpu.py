@@ -143,7 +143,7 @@ def test_lookup_gradient_of_many_slots(docs, vocab, hidden):
 
 
 @pytest.mark.parametrize("docs,cp,rank,vocab,hidden", [([16700], 1, 0, 33000, 64), ([2600, 400], 1, 0, 16400, 776), ([5000], 1, 0, 520, 2056),
-                                                       ([4900], 1, 0, 13000, 2048), ([16, 60], 1, 0, 40000, 72)])
+                                                       ([4900], 1, 0, 13000, 2048), ([16, 60], 1, 0, 40000, 72), ([31], 1, 0, 20000, 1032), ([9, 4], 1, 0, 70, 2048)])
 def test_loss_in_pieces_and_wide_tiles(docs, cp, rank, vocab, hidden):
     """Three pieces of the vocabulary; more tiles than compute units; a long sum along few words; tiles divided so that
     their parts take two rounds; few slots and many words."""
