@@ -443,11 +443,11 @@ def _vocab_call(name, desc, tensors, workspace=None):
     """One device call on the tensors' device and that device's current stream.  tensors: (tensor, dtype, shape) in the order of the C call.
     (Plain integers and the raw stream: with pointer and Stream objects a lookup took 13.5 us on the host, 7 us this way.)"""
     import torch
-    device = tensors[0][0].device
-    args = [C.byref(desc)]
+    device, args = None, [C.byref(desc)]
     for t, dtype, shape in tensors:
         if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous()):
             raise TypeError(f"{name}: expected a contiguous GPU tensor")
+        device = device or t.device
         if t.dtype != dtype:
             raise TypeError(f"{name}: expected dtype {dtype}, got {t.dtype}")
         if t.shape != shape:
@@ -507,8 +507,8 @@ class Vocabulary:
     """The two ends of a model on one rank's slots (q_idx and cu_seqlens_k of wlb_shard): the slots' rows of the table and the
     cross entropy of their next tokens, with gradients.  Owns the map on the device and a workspace for each kind of call,
     allocated with the first (make one before capturing it into a graph) and kept: calls of one kind must be ordered on their
-    stream(s).  All arithmetic is in libwlb.  `tokens` are the packed sequence's [t_kv] int32; the loss takes a copy
-    with values outside [0, vocab) where a token is not trained on."""
+    stream(s), and the object has to live as long as graphs that captured them.  All arithmetic is in libwlb.  `tokens` are
+    the packed sequence's [t_kv] int32; the loss takes a copy with values outside [0, vocab) where a token is not trained on."""
 
     def __init__(self, q_idx, cu_seqlens_k, vocab, hidden, embed_scale=1.0, logit_scale=1.0, device="cuda:0"):
         import torch
@@ -520,14 +520,24 @@ class Vocabulary:
         self.embed_desc = vocab_desc(*shape, scale=embed_scale)
         self.add_desc = vocab_desc(*shape, scale=embed_scale, flags=VOCAB_ACCUMULATE)
         self.loss_desc = vocab_desc(*shape, scale=logit_scale)
-        self.workspace = {}
+        self.device = self.q_idx.device
+        self.workspace, self.streams = {}, {}
 
-    def _room(self, kind):
-        """The workspace of calls of a kind: 0 embed_backward, 1 loss, 2 loss_backward."""
-        if kind not in self.workspace:
+    def _room(self, kind=None):
+        """The workspace of calls of a kind (None: it takes none): 0 embed_backward, 1 loss, 2 loss_backward.  What the object holds is kept from reuse,
+        once the object is gone, until the work on every stream that it was called on is done."""
+        if self.device.type == "cuda":
+            raw = self.torch._C._cuda_getCurrentRawStream(self.device.index)
+            if raw not in self.streams:
+                self.streams[raw] = self.torch.cuda.current_stream(self.device)
+                for t in (self.q_idx, self.cu_k, *self.workspace.values()):
+                    t.record_stream(self.streams[raw])
+        if kind is not None and kind not in self.workspace:
             nbytes = wlb_vocab_workspace_size(self.embed_desc)[kind]
             self.workspace[kind] = self.torch.empty(nbytes, dtype=self.torch.uint8, device=self.device)
-        return self.workspace[kind]
+            for stream in self.streams.values():
+                self.workspace[kind].record_stream(stream)
+        return self.workspace.get(kind)
 
     def _empty(self, shape, dtype=None):
         return self.torch.empty(shape, dtype=dtype or self.torch.bfloat16, device=self.device)
@@ -536,6 +546,7 @@ class Vocabulary:
         """-> x [n_q][hidden]: embed_scale * table[token of the slot], 0 for padding"""
         d = self.embed_desc
         x = self._empty((d.n_q, d.hidden)) if x is None else x
+        self._room()
         wlb_embed_fwd(d, tokens, self.q_idx, table, x)
         return x
 

@@ -315,3 +315,22 @@ def test_on_another_stream():
         got = ends.loss_backward(e.x, e.table, e.tokens, lse, e.d_loss)
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_workspace_is_kept_from_reuse_while_another_stream_works():
+    import torch
+    e = Ends(12, [600], 1, 0, 2000, 128)
+    side = torch.cuda.Stream()
+    ends = B.Vocabulary(e.q_idx, e.cu, e.vocab, e.hidden)
+    ends.loss(e.x, e.table, e.tokens)                       # the workspace belongs to the current stream
+    torch.cuda.synchronize()
+    nbytes, at = ends.workspace[1].numel(), ends.workspace[1].data_ptr()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)                      # about 0.1 s
+        loss, _ = ends.loss(e.x, e.table, e.tokens)
+    del ends
+    rooms = [torch.empty(nbytes, dtype=torch.uint8, device=DEV) for _ in range(4)]
+    busy = not side.query()
+    side.synchronize()
+    assert busy and at not in [r.data_ptr() for r in rooms]
+    assert torch.equal(loss, e.loss()[0])
