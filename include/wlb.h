@@ -383,7 +383,7 @@ wlb_status wlb_attn_bwd(const wlb_attn_desc* desc, const void* q, const void* k,
  *           value there, -1 say.  With l[i][v] = scale * <x[i], table[v]>:
  *           lse[i] = ln sum_v exp l[i][v],  loss[i] = lse[i] - l[i][target]  (float, natural logarithm).
  *           A slot without a target has loss 0 and lse -inf, its row of x is never used, whatever it holds, and its row of dx is 0.
- *           The logits are never kept: the forward leaves one maximum and one sum per slot and 256 words, the
+ *           The logits are never kept: the forward leaves one maximum and one sum per slot and 64 to 256 words, the
  *           backward computes them again for one piece of the vocabulary at a time.
  *
  * The gradients are those of sum_i d_loss[i] * loss[i] and of sum <dx, x>; dtable is THIS rank's partial sum (as dK / dV of
@@ -391,6 +391,7 @@ wlb_status wlb_attn_bwd(const wlb_attn_desc* desc, const void* q, const void* k,
  * floating-point atomics.  dx, dtable and x are rounded to bf16 once.  The logits' gradient, relative to the largest
  * |d_loss|, enters its two matrix products in bf16; where few slots leave these roundings nothing to average out with, what they
  * leave out is added (dx: at the targets, up to 128 slots; dtable: everywhere, up to 32).
+ * What a call writes overlaps neither what it reads nor its workspace.
  */
 typedef struct {
     int32_t n_q;       /* local slots (rows of x), >= 1                                          */

@@ -2,7 +2,7 @@
 // (wlb_loss_fwd / wlb_loss_bwd).
 //
 // With c = scale, l = <x, E_v> in fp32 sums of the MFMAs, n labelled slots:
-//   forward   one product l = X E^T.  A tile of 256 words x up to 256 slots leaves per slot its maximum and its sum of exp(c (l - max)), and the
+//   forward   one product l = X E^T.  A tile of up to 256 words and 256 slots leaves per slot its maximum and its sum of exp(c (l - max)), and the
 //             target's l where the tile holds it; loss_join_kernel combines a slot's tiles: lse = c max + ln sum, loss = c (max - l_t) + ln sum.
 //   backward  D = w (exp(c l - lse) - [v = target]) with w = d_loss / G, G the largest |d_loss|, in bf16, for one piece of the vocabulary at a
 //             time; then dE = c G D^T X for the piece's rows and dX += D E over the pieces, in fp32; dX is scaled by c G at the end.
@@ -20,7 +20,7 @@
 namespace wlb {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kWordTile = 256;                 // words (forward, D) and columns of hidden (dX) per tile
+constexpr int kWordTile = 256;                 // words (forward, D) and columns of hidden (dX) per tile; some tiles of few slots have less
 constexpr int kRowsThreads = 1024;
 
 // ------------------------------------------------------------------------------------------
@@ -164,7 +164,6 @@ struct Work : GemmGrid {
 
 // Joins the parts of divided tiles in order: f(tm, tn, n, m, four sums).  A row n of a tile is a wavefront's, of a narrow tile, which has up to kMaxParts parts, a
 // workgroup's, whose wavefronts add up a quarter of the parts each.
-template <class S> constexpr int join_rows() { return S::RING ? 4 : 1; }        // rows of a tile to a workgroup
 template <class S, class F>
 __device__ __forceinline__ void join_parts(const Work& w, const float* parts, F f) {
     static_assert(S::TM == 256, "four columns a lane");
