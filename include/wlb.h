@@ -383,7 +383,7 @@ wlb_status wlb_attn_bwd(const wlb_attn_desc* desc, const void* q, const void* k,
  *           value there, -1 say.  With l[i][v] = scale * <x[i], table[v]>:
  *           lse[i] = ln sum_v exp l[i][v],  loss[i] = lse[i] - l[i][target]  (float, natural logarithm).
  *           A slot without a target has loss 0 and lse -inf, its row of x is never used, whatever it holds, and its row of dx is 0.
- *           The logits are never kept: the forward leaves one maximum and one sum per slot and 64 to 256 words, the
+ *           The logits are never kept: the forward leaves one maximum and one sum per slot and 128 or 256 words, the
  *           backward computes them again for one piece of the vocabulary at a time.
  *
  * The gradients are those of sum_i d_loss[i] * loss[i] and of sum <dx, x>; dtable is THIS rank's partial sum (as dK / dV of

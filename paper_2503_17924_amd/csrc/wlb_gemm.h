@@ -27,20 +27,24 @@ __device__ __forceinline__ int swz_m(int r, int cc) { return cc ^ (((r & 3) << 2
 constexpr int kOutOfRange = (int)0xfffffff0u;      // a lane offset at which every buffer load returns 0
 constexpr uint32_t kMaxRecords = 0xffffffe0u;
 
-template <int WM_, int WN_, int BM_, int BN_, bool MP_, bool MQ_, int KS_ = kStepK>
+template <int WM_, int WN_, int BM_, int BN_, bool MP_, bool MQ_>
 struct GemmShape {
     static constexpr int WM = WM_, WN = WN_, BM = BM_, BN = BN_;         // wavefronts, and blocks of 16 of a wavefront
-    static constexpr int KS = KS_;                                       // k of a step
     static constexpr bool MP = MP_, MQ = MQ_;                            // operand kinds: m / n contiguous in memory
     static constexpr int TM = WM * BM * 16, TN = WN * BN * 16;
-    static constexpr int P_BYTES = TM * KS * 2, Q_BYTES = TN * KS * 2, STAGE = P_BYTES + Q_BYTES;
+    static constexpr int P_BYTES = TM * kStepK * 2, Q_BYTES = TN * kStepK * 2, STAGE = P_BYTES + Q_BYTES;
     static constexpr bool RING = TM == 256 && TN == 256;
+    // Three where both operands are of kind K: bound by the latency of the copies (33 slots, 32768 words, hidden 1024: D 13.5 us, with two 16.7; statistics of 128
+    // slots, 50000 words, hidden 1536: 58 and 65).  dX waits for memory that dE has just written (45 slots, 65536 words, hidden 2048: 80 us, with two 77.5),
+    // and dE keeps two workgroups to a compute unit (66 us, with three buffers and one 100).
+    static constexpr int stages() { return !MP && !MQ && 3 * STAGE + 4 * OUT_WAVE <= 163840 ? 3 : 2; }
     // a wavefront's output on its way to memory: 32 rows of its bf16 values, or of 64 floats where sums are kept in parts
     static constexpr int OUT_WAVE = RING || (MP && !MQ) ? 8192 : BM * 1024;
-    // five LDS slots of one operand's tile, one of them free for the output at an item's end; or two buffers of both tiles, and the output
-    static constexpr int LDS_BYTES = RING ? 5 * P_BYTES : 2 * STAGE + 4 * OUT_WAVE;
+    // five LDS slots of one operand's tile, one of them free for the output at an item's end; or STAGES buffers of both tiles, and the output
+    static constexpr int STAGES = RING ? 2 : stages();
+    static constexpr int LDS_BYTES = RING ? 5 * P_BYTES : STAGES * STAGE + 4 * OUT_WAVE;
     static constexpr int PER_CU = LDS_BYTES > 81920 || TN >= 128 && !MQ ? 1 : 2;        // workgroups to a compute unit
-    static_assert(WM * WN == 4 && (KS == kStepK || !(RING || MP || MQ)), "four wavefronts; long steps for narrow tiles of kind K");
+    static_assert(WM * WN == 4, "four wavefronts");
     static_assert(LDS_BYTES <= 163840, "LDS of a compute unit");
 };
 
@@ -114,19 +118,11 @@ struct GemmOperand {
     const int32_t* list;        // kind K: numbers of the rows counted from `at`, or null
 };
 
-// Place of 16-byte chunk cc of row r in an LDS tile of kind K whose rows hold KS values: 16 rows x one chunk, as the operands are read, lie in 16 different
-// chunks of 256 bytes.
-template <int KS>
-__device__ __forceinline__ int swz_k(int r, int cc) {
-    static_assert(KS == 64 || KS == 256, "rows of 128 or 512 bytes");
-    return KS == 64 ? swz<8>(r, cc) : cc ^ (r & 15);
-}
-
 // Copies of one operand's tile.  T: its width (rows of kind K, columns of kind M).
-template <int T, bool M, int KS>
+template <int T, bool M>
 struct TileCopy {
-    static constexpr int N = T * KS * 2 / 1024 / 4;             // 1 KiB instructions per wavefront and step
-    static constexpr int CH = M ? T / 8 : KS / 8;               // 16-byte chunks per LDS row
+    static constexpr int N = T * kStepK * 2 / 1024 / 4;             // 1 KiB instructions per wavefront and step
+    static constexpr int CH = M ? T / 8 : kStepK / 8;               // 16-byte chunks per LDS row
     static constexpr int RPI = 64 / CH;                         // LDS rows per instruction
     static_assert(N >= 1, "tile too narrow");
     int voff[N];
@@ -136,7 +132,7 @@ struct TileCopy {
     int wave, lane, left, turn;                                 // k that exist from this step's start on; where steps go on at k = 0, or 0
 
     __device__ __forceinline__ int row_of(int n) const { return (wave * N + n) * RPI + lane / CH; }
-    __device__ __forceinline__ int chunk_of(int n) const { return M ? swz_m(row_of(n), lane % CH) : swz_k<KS>(row_of(n), lane % CH); }
+    __device__ __forceinline__ int chunk_of(int n) const { return M ? swz_m(row_of(n), lane % CH) : swz<8>(row_of(n), lane % CH); }
     // ld: elements between rows
     __device__ __forceinline__ void init(long long ld, int wave_, int lane_) {
         row_bytes = (uint32_t)(ld * 2);
@@ -162,7 +158,7 @@ struct TileCopy {
         rs.r[2] = on ? (int)kMaxRecords : 0;
         rs.r[3] = 0x00020000;
         left = depth;
-        if (start) move(start * KS);
+        if (start) move(start * kStepK);
     }
     __device__ __forceinline__ void move(int k) {
         const uint64_t a = (((uint64_t)(uint32_t)rs.r[1] << 32) | (uint32_t)rs.r[0]) + (uint64_t)((long long)k * (M ? row_bytes : 2u));
@@ -170,10 +166,10 @@ struct TileCopy {
         rs.r[1] = (int)(uint32_t)(a >> 32);
         left -= k;
     }
-    __device__ __forceinline__ void next() { move(turn && left == KS ? KS - turn : KS); }
+    __device__ __forceinline__ void next() { move(turn && left == kStepK ? kStepK - turn : kStepK); }
     // in the last step of a tile: lanes whose k does not exist load zeros from here on
     __device__ __forceinline__ void cut() {
-        if (left >= KS) return;
+        if (left >= kStepK) return;
 #pragma unroll
         for (int n = 0; n < N; ++n)
             if ((M ? row_of(n) : chunk_of(n) * 8) >= left) voff[n] = kOutOfRange;
@@ -182,9 +178,9 @@ struct TileCopy {
 };
 
 // Operand fragments of a wavefront out of LDS: B blocks of 16 rows (columns).
-template <int T, int B, bool M, int KS>
+template <int T, int B, bool M>
 struct Fragments {
-    static constexpr int READS = M ? 2 * B : B, KN = KS / 32;
+    static constexpr int READS = M ? 2 * B : B, KN = kStepK / 32;
     uint32_t at[M ? B : KN];        // K: by 32-step, the blocks 16 rows apart; M: by block, the 32-steps 32 rows apart
 
     __device__ __forceinline__ void init(uint32_t tile, int first, int lane) {
@@ -197,7 +193,7 @@ struct Fragments {
         } else {
             const int row = first * 16 + lane % 16;
 #pragma unroll
-            for (int kk = 0; kk < KN; ++kk) at[kk] = tile + row * (KS * 2) + swz_k<KS>(row, 4 * kk + lane / 16) * 16;
+            for (int kk = 0; kk < KN; ++kk) at[kk] = tile + row * (kStepK * 2) + swz<8>(row, 4 * kk + lane / 16) * 16;
         }
     }
     __device__ __forceinline__ void move(int bytes) {
@@ -212,7 +208,7 @@ struct Fragments {
 #pragma unroll
             for (int e = 0; e < 4; ++e) f[i][4 * h + e] = v[e];
         } else {
-            f[r] = *reinterpret_cast<const WLB_LDS bf16x8*>((uintptr_t)(at[kk] + r * (16 * KS * 2)));
+            f[r] = *reinterpret_cast<const WLB_LDS bf16x8*>((uintptr_t)(at[kk] + r * (16 * kStepK * 2)));
         }
     }
 };
@@ -225,14 +221,14 @@ struct Gemm {
     f32x4 acc[S::BM][S::BN];    // register r of lane l: m = 16 i + (l/16)*4 + r, n = 16 j + l%16 of the wavefront's part
     int wave, lane, wm, wn;
     uint32_t lds;
-    TileCopy<S::TM, S::MP, S::KS> cp;
-    TileCopy<S::TN, S::MQ, S::KS> cq;
-    Fragments<S::TM, S::BM, S::MP, S::KS> fp;
-    Fragments<S::TN, S::BN, S::MQ, S::KS> fq;
+    TileCopy<S::TM, S::MP> cp;
+    TileCopy<S::TN, S::MQ> cq;
+    Fragments<S::TM, S::BM, S::MP> fp;
+    Fragments<S::TN, S::BN, S::MQ> fq;
     static constexpr int NP = decltype(cp)::N, NQ = decltype(cq)::N, RP = decltype(fp)::READS, RQ = decltype(fq)::READS;
 
-    // An item has two steps at least (the second may be zeros), so that the steps two ahead of its last two are the next item's first two.
-    static __device__ __forceinline__ int steps_of(const GemmItem& it) { return max((it.depth + S::KS - 1) / S::KS, 2); }
+    // An item has STAGES steps at least (later ones may be zeros), so that the steps that many ahead of its last ones are the next item's first.
+    static __device__ __forceinline__ int steps_of(const GemmItem& it) { return max((it.depth + kStepK - 1) / kStepK, S::STAGES); }
 
     __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -260,14 +256,14 @@ struct Gemm {
     // every row at a time, which few of the memory's channels hold (64K rows of 4096 bytes: a plain read in this order 4.1 TB/s, 5.5 with starts spread).
     __device__ __forceinline__ int start_of(const GemmItem& it) const {
         if constexpr (S::MP || S::MQ) return 0;
-        if (it.depth % S::KS != 0 || it.depth == 0) return 0;
-        return uniform(kTurn * it.tm % (it.depth / S::KS));
+        if (it.depth % kStepK != 0 || it.depth < S::STAGES * kStepK) return 0;
+        return uniform(kTurn * it.tm % (it.depth / kStepK));
     }
 
-    // Narrow tiles in two LDS buffers of both operands.  Here too copies go on from one item to the next while sums go to memory.
+    // Narrow tiles in STAGES LDS buffers of both operands.  Here too copies go on from one item to the next while sums go to memory.
     template <class Work, class Done>
     __device__ __forceinline__ void pair(const Work& work, const Done& done) {
-        constexpr int BM = S::BM, BN = S::BN, KN = S::KS / 32;
+        constexpr int BM = S::BM, BN = S::BN, KN = kStepK / 32, ST = S::STAGES;
         GemmItem it, next = {};
         if (!work.item((int)blockIdx.x, 0, it)) return;
         cp.tile(work.p(it));
@@ -275,7 +271,7 @@ struct Gemm {
         fp.init(lds, wm * BM, lane);
         fq.init(lds + S::P_BYTES, wn * BN, lane);
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
+        for (int s = 0; s < ST; ++s) {
             if (s) { cp.next(); cq.next(); }
             else { cp.first(it.depth, true, start_of(it)); cq.first(it.depth, true, start_of(it)); }
             cp.cut();
@@ -286,7 +282,7 @@ struct Gemm {
             for (int n = 0; n < NQ; ++n) cq.issue(n, lds + s * S::STAGE + S::P_BYTES);
         }
         bf16x8 a[2][BM], b[2][BN];
-        wait_vmem_le<NP + NQ>();
+        wait_vmem_le<(ST - 1) * (NP + NQ)>();
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < RP; ++r) fp.read(r, 0, a[0]);
@@ -308,9 +304,9 @@ struct Gemm {
                     if (then == 0) {
                         // the step's last operands are in registers and the next step's tiles in LDS, for every wavefront
                         wait_lds();
-                        wait_vmem();
+                        wait_vmem_le<(ST - 2) * (NP + NQ)>();
                         __syncthreads();
-                        if (s + 2 == steps) {
+                        if (s + ST == steps) {
                             if (more) { cp.tile(next_p); cq.tile(next_q); }
                             const int start = more ? start_of(next) : 0;
                             cp.first(next.depth, more, start);
@@ -321,14 +317,14 @@ struct Gemm {
                         }
                         cp.cut();
                         cq.cut();
-                        const int flip = buffer ? -S::STAGE : S::STAGE;
-                        fp.move(flip);
-                        fq.move(flip);
-                        buffer ^= 1;
+                        const int on = buffer < ST - 1 ? 1 : 1 - ST;
+                        fp.move(on * S::STAGE);
+                        fq.move(on * S::STAGE);
+                        buffer += on;
                     }
 #pragma unroll
                     for (int x = 0; x < BM * BN || x < RP + RQ || (then == 0 && x < NP + NQ); ++x) {
-                        // reads of the operands of the next 32-step, copies of the step after the next, MFMAs of this one
+                        // reads of the operands of the next 32-step, copies of the step STAGES on, MFMAs of this one
                         if (x < RQ) fq.read(x, then, b[then & 1]);
                         else if (x < RP + RQ) fp.read(x - RQ, then, a[then & 1]);
                         if (then == 0) {
@@ -343,7 +339,7 @@ struct Gemm {
                     }
                 }
             }
-            done(*this, it, ahead, lds + 2 * S::STAGE);
+            done(*this, it, ahead, lds + ST * S::STAGE);
             wait_lds();
             if (!more) break;
             it = next;

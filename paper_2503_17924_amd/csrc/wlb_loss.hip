@@ -672,9 +672,6 @@ template <bool MP, bool MQ> using Slots32 = GemmShape<4, 1, 4, 2, MP, MQ>;
 using Slots128Low = GemmShape<4, 1, 2, 8, false, false>;
 using Slots64Low = GemmShape<4, 1, 2, 4, false, false>;
 using Slots32Low = GemmShape<4, 1, 2, 2, false, false>;
-// 64 words in steps of 256: the memory gives pieces of 512 bytes of a table's rows faster than pieces of 128 (a plain read 5.3 and 4.3 TB/s)
-using Slots32Long = GemmShape<4, 1, 1, 2, false, false, 256>;
-constexpr int kLongHidden = 1024;
 
 static int slot_tile(int n_q) { return n_q <= 32 ? 32 : n_q <= 64 ? 64 : n_q <= 128 ? 128 : 256; }
 
@@ -701,9 +698,7 @@ static LossLayout loss_layout(const wlb_vocab_desc& d) {
     L.blocks = (d.n_q + kRowsThreads - 1) / kRowsThreads;
     L.tile = slot_tile(d.n_q);
     // Few slots: tiles of 128 words where those of 256 are fewer than the compute units (32768 words, hidden 1024, 65 slots: statistics 19 us, with 256 33).
-    // Up to 32 slots: of 64, where rows hold four long steps (131072 words, hidden 2048, 20 slots: 108 us, with 256 126; 50000 words, hidden 512: 16 and 11).
-    L.word_tile = L.tile == 32 && d.hidden >= kLongHidden ? kWordTile / 4
-                  : L.tile < 256 && (d.vocab + kWordTile - 1) / kWordTile < compute_units() ? kWordTile / 2 : kWordTile;
+    L.word_tile = L.tile < 256 && (d.vocab + kWordTile - 1) / kWordTile < compute_units() ? kWordTile / 2 : kWordTile;
     L.word_tiles = (d.vocab + L.word_tile - 1) / L.word_tile;
     L.pitch_rows = (int)align_up(n_q, 64);
     const size_t words = align_up(v, kWordTile);
@@ -746,7 +741,7 @@ static wlb_status check_loss(const wlb_vocab_desc* desc, const char* call) {
     // rows of x are addressed with 32-bit offsets
     if ((uint64_t)desc->n_q * desc->hidden * 2 >= (1ull << 32) - (1u << 20))
         return fail(WLB_ERR_UNSUPPORTED, "%s: x of 4 GiB or more is not supported", call);
-    if ((int64_t)(desc->vocab / (kWordTile / 4) + 1) * (desc->n_q / 32 + 1) > (1 << 30))
+    if ((int64_t)(desc->vocab / (kWordTile / 2) + 1) * (desc->n_q / 32 + 1) > (1 << 30))
         return fail(WLB_ERR_UNSUPPORTED, "%s: vocab=%d words for n_q=%d slots", call, desc->vocab, desc->n_q);
     return WLB_OK;
 }
@@ -834,8 +829,7 @@ extern "C" wlb_status wlb_loss_fwd(const wlb_vocab_desc* desc, const void* x, co
     a.vocab = d.vocab; a.hidden = d.hidden; a.pitch = L.pitch_rows; a.c2 = d.scale * kLog2e;
     a.parts = (float*)(ws + L.off_parts);
     const bool low = L.word_tile < kWordTile;
-    if (L.word_tile == kWordTile / 4) launch_narrow<Slots32Long>(loss_stats_kernel<Slots32Long>, a, L.word_tiles, stream);
-    else if (L.tile == 32) low ? launch_narrow<Slots32Low>(loss_stats_kernel<Slots32Low>, a, L.word_tiles, stream)
+    if (L.tile == 32) low ? launch_narrow<Slots32Low>(loss_stats_kernel<Slots32Low>, a, L.word_tiles, stream)
                            : launch_narrow<Slots32<false, false>>(loss_stats_kernel<Slots32<false, false>>, a, L.word_tiles, stream);
     else if (L.tile == 64) low ? launch_narrow<Slots64Low>(loss_stats_kernel<Slots64Low>, a, L.word_tiles, stream)
                            : launch_narrow<Slots64<false, false>>(loss_stats_kernel<Slots64<false, false>>, a, L.word_tiles, stream);
@@ -882,8 +876,7 @@ extern "C" wlb_status wlb_loss_bwd(const wlb_vocab_desc* desc, const void* x, co
         a.final = p == L.pieces - 1;
         const int word_tiles = (a.piece_n + kWordTile - 1) / kWordTile, column_tiles = (d.hidden + kWordTile - 1) / kWordTile;
         const int few_tiles = (a.piece_n + L.word_tile - 1) / L.word_tile;
-        if (L.word_tile == kWordTile / 4) launch_narrow<Slots32Long>(loss_d_kernel<Slots32Long>, a, few_tiles, stream);
-        else if (L.tile == 32) low ? launch_narrow<Slots32Low>(loss_d_kernel<Slots32Low>, a, few_tiles, stream)
+        if (L.tile == 32) low ? launch_narrow<Slots32Low>(loss_d_kernel<Slots32Low>, a, few_tiles, stream)
                                : launch_narrow<Slots32<false, false>>(loss_d_kernel<Slots32<false, false>>, a, few_tiles, stream);
         else if (L.tile == 64) low ? launch_narrow<Slots64Low>(loss_d_kernel<Slots64Low>, a, few_tiles, stream)
                                : launch_narrow<Slots64<false, false>>(loss_d_kernel<Slots64<false, false>>, a, few_tiles, stream);
