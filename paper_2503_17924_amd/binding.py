@@ -522,12 +522,13 @@ class Vocabulary:
         self.loss_desc = vocab_desc(*shape, scale=logit_scale)
         self.device = self.q_idx.device
         self.workspace, self.streams = {}, {}
+        self._raw_stream = torch._C._cuda_getCurrentRawStream if self.device.type == "cuda" else None
 
     def _room(self, kind=None):
         """The workspace of calls of a kind (None: it takes none): 0 embed_backward, 1 loss, 2 loss_backward.  What the object holds is kept from reuse,
         once the object is gone, until the work on every stream that it was called on is done."""
-        if self.device.type == "cuda":
-            raw = self.torch._C._cuda_getCurrentRawStream(self.device.index)
+        if self._raw_stream:
+            raw = self._raw_stream(self.device.index)
             if raw not in self.streams:
                 self.streams[raw] = self.torch.cuda.current_stream(self.device)
                 for t in (self.q_idx, self.cu_k, *self.workspace.values()):
