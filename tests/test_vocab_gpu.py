@@ -150,6 +150,13 @@ def test_loss_in_pieces_and_wide_tiles(docs, cp, rank, vocab, hidden):
     Ends(4, docs, cp, rank, vocab, hidden).check_loss()
 
 
+@pytest.mark.parametrize("slots", [20, 60, 120])
+@pytest.mark.parametrize("vocab,hidden", [(1000, 128), (1000, 192), (1000, 256), (777, 960), (70001, 192), (70001, 320), (140000, 256)])
+def test_few_slots_whose_tiles_start_at_different_steps(slots, vocab, hidden):
+    """Columns of two steps, of as many as there are buffers, and more; one tile to a workgroup and several."""
+    Ends(5, [slots], 1, 0, vocab, hidden).check_loss()
+
+
 def test_every_slot_without_a_target():
     import torch
     e = Ends(5, [1] * 70, 1, 0, 500, 64)
