@@ -619,7 +619,10 @@ __device__ __forceinline__ void put_dx(const GradArgs& a, float factor, int n_ro
         const bf16x4 e = *reinterpret_cast<const bf16x4*>(a.table + (size_t)a.target[row] * a.hidden + col);
         const float rest = a.target_rest[row];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] += rest * (float)e[k];
+        for (int k = 0; k < 4; ++k) {
+            const float more = rest * (float)e[k];
+            v[k] += __builtin_isfinite(more) ? more : 0.f;       // beside an entry that is not finite the sum is what it is already
+        }
     }
     if (a.final) *reinterpret_cast<bf16x4*>(a.dx + (size_t)a.rows[row] * a.hidden + col) = pack4(factor * v[0], factor * v[1], factor * v[2], factor * v[3]);
     else *sum = v;
