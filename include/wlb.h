@@ -382,6 +382,8 @@ wlb_status wlb_attn_bwd(const wlb_attn_desc* desc, const void* q, const void* k,
  *           word; a caller that does not train on some tokens (prompts) passes a copy of the sequence that has another
  *           value there, -1 say.  With l[i][v] = scale * <x[i], table[v]>:
  *           lse[i] = ln sum_v exp l[i][v],  loss[i] = lse[i] - l[i][target]  (float, natural logarithm).
+ *           Infinite logits (and those that are not floats once they are taken times log2 e) mean what the formulas
+ *           make of them: lse and loss are +inf beside a word's +inf, loss is NaN where that is the target's, +inf where the target's is -inf.
  *           A slot without a target has loss 0 and lse -inf, its row of x is never used, whatever it holds, and its row of dx is 0.
  *           The logits are never kept: the forward leaves one maximum and one sum per slot and 128 or 256 words, the
  *           backward computes them again for one piece of the vocabulary at a time.

@@ -198,7 +198,12 @@ __device__ __forceinline__ void join_parts(const Work& w, const float* parts, F 
 
 // ------------------------------------------------------------------------------------------
 // Forward.  Exponents are in units of log2, relative to a tile's reference: its largest l times c2, rounded.  What the rounding
-// is off by cancels, since the reference is what the sum is stored with.
+// is off by cancels, since the reference is what the sum is stored with.  An infinite reference cannot be subtracted: there the exponents are taken as they
+// are, and 2^inf stays in the sum (a logit of +inf), or nothing does (all of them -inf, or words past the end).
+__device__ __forceinline__ float subtracted(float ref) { return __builtin_isinf(ref) ? 0.f : ref; }
+// a tile's sum, relative to a reference that is at least the tile's
+__device__ __forceinline__ float rescaled(float2 part, float ref) { return part.x == ref ? part.y : part.y * fast_exp2(part.x - ref); }
+
 struct StatsArgs {
     const __bf16 *x, *table;
     const int32_t *rows, *target, *count;
@@ -294,7 +299,7 @@ struct StatsDone {
                     }
                 if (mine) a.target_logit[n0 + n] = l;
             }
-            const float ref = top == -INFINITY ? -INFINITY : top * a.c2, from = top == -INFINITY ? 0.f : ref;    // a wavefront all of whose words lie past the end
+            const float ref = top * a.c2, from = subtracted(ref);
             float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < S::BM; ++i)
@@ -320,10 +325,7 @@ struct StatsDone {
 #pragma unroll
             for (int k = 1; k < S::WM; ++k) ref = fmaxf(ref, s_part[k * S::TN + n].x);
 #pragma unroll
-            for (int k = 0; k < S::WM; ++k) {
-                const float2 p = s_part[k * S::TN + n];
-                sum += p.x == -INFINITY ? p.y : p.y * fast_exp2(p.x - ref);      // p.y is 0 where every word lies past the end, or NaN
-            }
+            for (int k = 0; k < S::WM; ++k) sum += rescaled(s_part[k * S::TN + n], ref);
             a.part[(size_t)it.tm * a.pitch + n0 + n] = float2{ref, sum};
         }
         __syncthreads();
@@ -351,7 +353,7 @@ __global__ void __launch_bounds__(256) loss_stats_parts_kernel(StatsArgs a) {
         for (int k = 0; k < 4; ++k) most = word + k < a.vocab ? fmaxf(most, l[k]) : most;
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
-        const float ref = most == -INFINITY ? -INFINITY : most * a.c2, from = most == -INFINITY ? 0.f : ref;
+        const float ref = most * a.c2, from = subtracted(ref);
         const int t = a.target[row] - word;
         float sum = 0.f;
 #pragma unroll
@@ -384,9 +386,9 @@ __global__ void __launch_bounds__(256) loss_join_kernel(const float2* part, cons
             float r = ref;
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) r = fmaxf(r, p[k].x);
-            sum = ref == -INFINITY ? sum : sum * fast_exp2(ref - r);
+            sum = rescaled(float2{ref, sum}, r);
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) sum += p[k].x == -INFINITY ? p[k].y : p[k].y * fast_exp2(p[k].x - r);
+            for (int k = 0; k < kAhead; ++k) sum += rescaled(p[k], r);
             ref = r;
         }
     s_part[y][x] = float2{ref, sum};
@@ -394,10 +396,7 @@ __global__ void __launch_bounds__(256) loss_join_kernel(const float2* part, cons
     if (y != 0 || row >= n_rows) return;
     for (int k = 1; k < W; ++k) ref = fmaxf(ref, s_part[k][x].x);
     sum = 0.f;
-    for (int k = 0; k < W; ++k) {
-        const float2 p = s_part[k][x];
-        sum += p.x == -INFINITY ? p.y : p.y * fast_exp2(p.x - ref);
-    }
+    for (int k = 0; k < W; ++k) sum += rescaled(s_part[k][x], ref);
     const float log_sum = log2f(sum);
     const int slot = rows[row];
     lse[slot] = kLn2 * (ref + log_sum);
