@@ -391,8 +391,8 @@ wlb_status wlb_attn_bwd(const wlb_attn_desc* desc, const void* q, const void* k,
  * The gradients are those of sum_i d_loss[i] * loss[i] and of sum <dx, x>; dtable is THIS rank's partial sum (as dK / dV of
  * the attention).  Sums are held in 32 bits and in an order that the sizes alone decide: deterministic, no
  * floating-point atomics.  dx, dtable and x are rounded to bf16 once.  The logits' gradient, relative to the largest
- * |d_loss|, enters its two matrix products in bf16; where few slots leave these roundings nothing to average out with, what they
- * leave out is added (dx: at the targets, up to 128 slots; dtable: everywhere, up to 32).
+ * |d_loss|, enters its two matrix products in bf16.  What that leaves out at the targets is added to dx; where up to 32 slots have a
+ * target, whose roundings find little to average out with, all that it leaves out is added to dtable.
  * What a call writes overlaps neither what it reads nor its workspace.
  */
 typedef struct {

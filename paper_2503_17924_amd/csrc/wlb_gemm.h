@@ -463,7 +463,8 @@ struct Gemm {
     }
 
     // Rows of output through LDS, so that memory sees whole 256-byte pieces: 32 rows n at a time (16 where there are no more), `Bytes` = 2 (bf16: all of the
-    // wavefront's values of a row) or 4 (fp32: up to 64 of them).  value(i, j, r) gives the values; put(n, m, bits) takes 16 bytes: n, m counted in the tile.
+    // wavefront's values of a row) or 4 (fp32: up to 64 of them).  value(i, j, r) gives the values; put(n, m, bits, j) takes 16 bytes: n, m counted in the tile, n
+    // in one of the two blocks from j on.
     // mend(j, set): before a bf16 block j leaves, the lane may set(m, value) of its row n = lane % 16, m counted in the wavefront's part.
     struct NoMend { template <class Set> __device__ __forceinline__ void operator()(int, Set) const {} };
     template <int Bytes, class V, class Put, class Mend = NoMend>
@@ -472,6 +473,8 @@ struct Gemm {
         constexpr int ROWB = G * 16 * Bytes, CH = ROWB / 16, RPI = 64 / CH;                      // bytes, chunks of a row; rows per pass
         static_assert(S::BM % G == 0 && S::BN % H == 0 && ROWB <= 256 && 16 * H % RPI == 0, "whole passes");
         const uint32_t mine = room + wave * S::OUT_WAVE;
+        int l = lane;
+        asm volatile("" : "+v"(l));         // addresses are made here: made in front of all items, they take registers that the steps need
 #pragma unroll
         for (int j0 = 0; j0 < S::BN; j0 += H)
 #pragma unroll
@@ -480,7 +483,7 @@ struct Gemm {
                 for (int j = 0; j < H; ++j)
 #pragma unroll
                     for (int i = 0; i < G; ++i) {
-                        const int row = j * 16 + lane % 16, byte = (i * 16 + (lane / 16) * 4) * Bytes;
+                        const int row = j * 16 + l % 16, byte = (i * 16 + (l / 16) * 4) * Bytes;
                         const uint32_t to = mine + row * ROWB + (((byte / 16) ^ (row & (CH - 1))) * 16) + byte % 16;
                         const float v0 = value(i0 + i, j0 + j, 0), v1 = value(i0 + i, j0 + j, 1), v2 = value(i0 + i, j0 + j, 2), v3 = value(i0 + i, j0 + j, 3);
                         if (Bytes == 2) *reinterpret_cast<WLB_LDS bf16x4*>((uintptr_t)to) = pack4(v0, v1, v2, v3);
@@ -491,16 +494,16 @@ struct Gemm {
 #pragma unroll
                     for (int j = 0; j < H; ++j)
                         mend(j0 + j, [&](int m, float v) __attribute__((always_inline)) {
-                            const int row = j * 16 + lane % 16;
+                            const int row = j * 16 + l % 16;
                             *reinterpret_cast<WLB_LDS __bf16*>((uintptr_t)(mine + row * ROWB + (((m * 2 / 16) ^ (row & (CH - 1))) * 16) + m * 2 % 16)) = (__bf16)v;
                         });
                 }
                 asm volatile("" ::: "memory");      // LDS takes a wavefront's accesses in their order
 #pragma unroll
                 for (int t = 0; t < 16 * H / RPI; ++t) {
-                    const int n = t * RPI + lane / CH, c = lane % CH;
+                    const int n = t * RPI + l / CH, c = l % CH;
                     const i32x4 v = *reinterpret_cast<const WLB_LDS i32x4*>((uintptr_t)(mine + n * ROWB + ((c ^ (n & (CH - 1))) * 16)));
-                    put(wn * (S::BN * 16) + j0 * 16 + n, wm * (S::BM * 16) + i0 * 16 + c * 16 / Bytes, v);
+                    put(wn * (S::BN * 16) + j0 * 16 + n, wm * (S::BM * 16) + i0 * 16 + c * 16 / Bytes, v, j0);
                 }
                 asm volatile("" ::: "memory");
                 __builtin_amdgcn_sched_barrier(0);
@@ -512,7 +515,7 @@ struct Gemm {
     __device__ __forceinline__ void part_out(uint32_t room, float* to, int rows) {
         static_assert(S::OUT_WAVE == 8192, "32 rows of 64 floats");
         rows_out<4>(room, [&](int i, int j, int r) __attribute__((always_inline)) { return sum(i, j, r); },
-                    [&](int n, int m, const i32x4& v) __attribute__((always_inline)) { if (S::RING || n < rows) *reinterpret_cast<i32x4*>(to + n * S::TM + m) = v; });
+                    [&](int n, int m, const i32x4& v, int) __attribute__((always_inline)) { if (S::RING || n < rows) *reinterpret_cast<i32x4*>(to + n * S::TM + m) = v; });
     }
 };
 

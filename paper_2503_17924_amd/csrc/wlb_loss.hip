@@ -6,7 +6,9 @@
 //             target's l where the tile holds it; loss_join_kernel combines a slot's tiles: lse = c max + ln sum, loss = c (max - l_t) + ln sum.
 //   backward  D = w (exp(c l - lse) - [v = target]) with w = d_loss / G, G the largest |d_loss|, in bf16, for one piece of the vocabulary at a
 //             time; then dE = c G D^T X for the piece's rows and dX += D E over the pieces, in fp32; dX is scaled by c G at the end.
-//             G keeps the factor that most training steps have in common (1 / tokens) out of the rounding of D.
+//             G keeps the factor that most training steps have in common (1 / tokens) out of the rounding of D.  What bf16 leaves out of D at a row's
+//             target, the largest of its entries, is added to dX in fp32.  In dE the roundings of many rows average out; up to kExactRows rows, which fill
+//             half of a step of its sum, D has a second set of rows with all that bf16 leaves out of the first.
 // Slots without a target are left out of everything: the others are listed in order (rows), and products run over that list.
 // Bound by the matrix products: 2 n V H operations forward, 6 n V H backward, where 64 slots or more share the table's
 // rows; by the table's bytes below that.
@@ -22,6 +24,18 @@ namespace wlb {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kWordTile = 256;                 // words (forward, D) and columns of hidden (dX) per tile; some tiles of few slots have less
 constexpr int kRowsThreads = 1024;
+constexpr int kExactRows = kStepK / 2;         // labelled slots up to which D has a second set of rows
+
+// Tiles.  `Slots32` .. `Slots128` serve calls of few slots: four wavefronts side by side along the words (or columns).
+template <bool MP, bool MQ> using Wide = GemmShape<2, 2, 8, 8, MP, MQ>;
+template <bool MP, bool MQ> using Half = GemmShape<2, 2, 4, 4, MP, MQ>;
+template <bool MP, bool MQ> using Slots128 = GemmShape<4, 1, 4, 8, MP, MQ>;
+template <bool MP, bool MQ> using Slots64 = GemmShape<4, 1, 4, 4, MP, MQ>;
+template <bool MP, bool MQ> using Slots32 = GemmShape<4, 1, 4, 2, MP, MQ>;
+// the same with tiles of 128 words
+using Slots128Low = GemmShape<4, 1, 2, 8, false, false>;
+using Slots64Low = GemmShape<4, 1, 2, 4, false, false>;
+using Slots32Low = GemmShape<4, 1, 2, 2, false, false>;
 
 // ------------------------------------------------------------------------------------------
 // The labelled slots.
@@ -404,9 +418,9 @@ __global__ void __launch_bounds__(256) loss_join_kernel(const float2* part, cons
 }
 
 // ------------------------------------------------------------------------------------------
-// Backward.  The labelled rows of x one behind the other (and once more, for D's second set of rows), and zeros in dx of the other slots.
+// Backward.  The labelled rows of x one behind the other (few of them once more, for D's second set of rows), and zeros in dx of the other slots.
 __global__ void __launch_bounds__(256) loss_gather_kernel(const uint4* x, uint4* rows_x, uint4* dx, const int32_t* rows, const int32_t* slot_target,
-                                                          const int32_t* count, int n_q, int chunks, int twice) {
+                                                          const int32_t* count, int n_q, int chunks) {
     const int i = (int)blockIdx.x * 4 + ((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (i >= n_q) return;
     const int n = *count;
@@ -414,15 +428,15 @@ __global__ void __launch_bounds__(256) loss_gather_kernel(const uint4* x, uint4*
     const size_t from = row ? (size_t)rows[i] * chunks : 0;
     for (int c = lane; c < chunks; c += 64) {
         if (row) rows_x[(size_t)i * chunks + c] = x[from + c];
-        if (row && twice) rows_x[(size_t)(n + i) * chunks + c] = x[from + c];
+        if (row && n <= kExactRows) rows_x[(size_t)(n + i) * chunks + c] = x[from + c];
         if (none) dx[(size_t)i * chunks + c] = uint4{0, 0, 0, 0};
     }
 }
 
 struct GradArgs {
     const __bf16 *table;
-    __bf16 *rows_x;                  // [labelled][hidden]
-    __bf16 *d;                       // [labelled][pitch]: D of the piece
+    __bf16 *rows_x;                  // [labelled][hidden], up to kExactRows rows twice
+    __bf16 *d;                       // [labelled][pitch]: D of the piece; behind up to kExactRows rows what bf16 leaves out of them
     __bf16 *dx, *dtable;
     float *dx_sum;                   // [n_q][hidden]: dX of the pieces so far, where there are several
     float *parts;                    // divided tiles
@@ -432,7 +446,6 @@ struct GradArgs {
     int vocab, hidden, n_q, pitch, workgroups;
     int piece0, piece_n;             // words of the piece
     int add, final;                  // dX: there are earlier pieces; this piece is the last
-    int twice;                       // D has a second set of rows, with what bf16 leaves out of the first
     float c2;
 };
 
@@ -483,7 +496,7 @@ struct DDone {
                     const float e = weight[j] * share(g.sum(i, j, r), j);
                     return edge && first + i * 16 + r >= a.piece_n ? 0.f : e;
                 },
-                [&](int n, int m, const i32x4& v) __attribute__((always_inline)) {
+                [&](int n, int m, const i32x4& v, int) __attribute__((always_inline)) {
                     if (n0 + n < w.qn) *reinterpret_cast<i32x4*>(a.d + (size_t)(n0 + n) * a.pitch + m0 + m) = v;
                 },
                 // the few targets among the words, from the unrounded probability (comparing every word with its row's target took 2.7 us a tile)
@@ -503,16 +516,16 @@ struct DDone {
                     if (!mine) return;
                     const float d = weight[j] * (share(l, j) - 1.f);
                     set(t + (g.lane / 16) * 4, d);
-                    if (!S::RING) a.target_rest[n0 + g.wn * (S::BN * 16) + j * 16 + g.lane % 16] = d - (float)(__bf16)d;
+                    a.target_rest[n0 + g.wn * (S::BN * 16) + j * 16 + g.lane % 16] = d - (float)(__bf16)d;
                 });
-            if (S::RING || !a.twice) return;
+            if (S::RING || w.qn > kExactRows) return;
             g.template rows_out<2>(
                 room,
                 [&](int i, int j, int r) __attribute__((always_inline)) {
                     const float p = share(g.sum(i, j, r), j), d = weight[j] * (target[j] == i * 16 + r ? p - 1.f : p);
                     return edge && first + i * 16 + r >= a.piece_n ? 0.f : d - (float)(__bf16)d;
                 },
-                [&](int n, int m, const i32x4& v) __attribute__((always_inline)) {
+                [&](int n, int m, const i32x4& v, int) __attribute__((always_inline)) {
                     if (n0 + n < w.qn) *reinterpret_cast<i32x4*>(a.d + (size_t)(w.qn + n0 + n) * a.pitch + m0 + m) = v;
                 });
         };
@@ -525,6 +538,18 @@ struct DDone {
 template <class S>
 __global__ void __launch_bounds__(256, S::PER_CU) loss_d_kernel(GradArgs a) {
     __shared__ __attribute__((aligned(1024))) char smem[S::LDS_BYTES];
+    if constexpr (S::RING) {
+        // few labelled slots among many: a wide tile's end with a second set of rows took twice as long, also for the calls that have none (16408 slots, 65536
+        // words, hidden 4096: 1795 us a piece, without it 1620)
+        using Few = Slots32<false, false>;
+        static_assert(Few::TN >= kExactRows && Few::LDS_BYTES <= S::LDS_BYTES, "one tile along the rows, in the same LDS");
+        if (ld_const(a.count) <= kExactRows) {
+            const Work w = d_work<Few>(a);
+            Gemm<Few> gemm;
+            gemm.run(smem, w, DDone<Few>{a, w});
+            return;
+        }
+    }
     const Work w = d_work<S>(a);
     Gemm<S> gemm;
     gemm.run(smem, w, DDone<S>{a, w});
@@ -533,6 +558,7 @@ __global__ void __launch_bounds__(256, S::PER_CU) loss_d_kernel(GradArgs a) {
 template <class S>
 __global__ void __launch_bounds__(256) loss_d_parts_kernel(GradArgs a) {
     const Work w = d_work<S>(a);
+    if (w.qn <= kExactRows) return;
     join_parts<S>(w, a.parts, [&](int tm, int tn, int n, int m, const f32x4& l) __attribute__((always_inline)) {
         const int row = tn * S::TN + n, word = tm * S::TM + m;
         if (row >= w.qn) return;
@@ -543,6 +569,7 @@ __global__ void __launch_bounds__(256) loss_d_parts_kernel(GradArgs a) {
         for (int k = 0; k < 4; ++k) {
             const float p = word + k < a.piece_n ? fast_exp2(__builtin_fmaf(l[k], a.c2, -lse2)) : 0.f;
             d[k] = weight * (t == k ? p - 1.f : p);
+            if (t == k) a.target_rest[row] = d[k] - (float)(__bf16)d[k];
         }
         *reinterpret_cast<bf16x4*>(a.d + (size_t)row * a.pitch + word) = pack4(d[0], d[1], d[2], d[3]);
     });
@@ -551,7 +578,8 @@ __global__ void __launch_bounds__(256) loss_d_parts_kernel(GradArgs a) {
 // dE of the piece: D^T X, both operands with the sum's index (the row) outermost.
 template <class S>
 __device__ __forceinline__ Work dtable_work(const GradArgs& a) {
-    return Work::make<S>(a.rows_x, a.hidden, a.hidden, a.d, a.pitch, a.piece_n, nullptr, ld_const(a.count) * (a.twice ? 2 : 1), a.workgroups, kNever);
+    const int n = ld_const(a.count);
+    return Work::make<S>(a.rows_x, a.hidden, a.hidden, a.d, a.pitch, a.piece_n, nullptr, n <= kExactRows ? 2 * n : n, a.workgroups, kNever);
 }
 
 struct NothingAhead {
@@ -574,7 +602,7 @@ struct DtableDone : NothingAhead {
             }
         const int m0 = it.tm * S::TM, n0 = it.tn * S::TN;
         g.template rows_out<2>(room, [&](int i, int j, int r) __attribute__((always_inline)) { return factor * g.sum(i, j, r); },
-                               [&](int n, int m, const i32x4& v) __attribute__((always_inline)) {
+                               [&](int n, int m, const i32x4& v, int) __attribute__((always_inline)) {
                                    if (n0 + n < a.piece_n && m0 + m < a.hidden)
                                        *reinterpret_cast<i32x4*>(a.dtable + (size_t)(a.piece0 + n0 + n) * a.hidden + m0 + m) = v;
                                });
@@ -607,24 +635,22 @@ __device__ __forceinline__ Work dx_work(const GradArgs& a) {
     return Work::make<S>(a.table + (size_t)a.piece0 * a.hidden, a.hidden, a.hidden, a.d, a.pitch, ld_const(a.count), nullptr, a.piece_n, a.workgroups, kNarrowParts);
 }
 
-// Rest: with what bf16 left out of D at the row's target, the largest of its entries: of many rows these roundings average out, in
-// few they show (one row: up to 2^-8 of all its gradient).
-template <bool Rest>
-__device__ __forceinline__ void put_dx(const GradArgs& a, float factor, int n_rows, int row, int col, f32x4 v) {
-    if (row >= n_rows || col >= a.hidden) return;
+// In the last piece with what bf16 left out of D at the row's target, the largest of its entries and a rounding that nothing in the row averages out with
+// (up to 2^-8 of all its gradient).  slot, target, rest: the row's, used in the last piece alone.
+__device__ __forceinline__ void put_dx(const GradArgs& a, float factor, int row, int col, f32x4 v, int slot, int target, float rest) {
     f32x4* sum = reinterpret_cast<f32x4*>(a.dx_sum + (size_t)row * a.hidden + col);
     if (a.add) v += *sum;
-    if (Rest && a.final) {
-        const bf16x4 e = *reinterpret_cast<const bf16x4*>(a.table + (size_t)a.target[row] * a.hidden + col);
-        const float rest = a.target_rest[row];
+    if (a.final) {
+        const bf16x4 e = *reinterpret_cast<const bf16x4*>(a.table + (size_t)target * a.hidden + col);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const float more = rest * (float)e[k];
             v[k] += __builtin_isfinite(more) ? more : 0.f;       // beside an entry that is not finite the sum is what it is already
         }
+        *reinterpret_cast<bf16x4*>(a.dx + (size_t)slot * a.hidden + col) = pack4(factor * v[0], factor * v[1], factor * v[2], factor * v[3]);
+    } else {
+        *sum = v;
     }
-    if (a.final) *reinterpret_cast<bf16x4*>(a.dx + (size_t)a.rows[row] * a.hidden + col) = pack4(factor * v[0], factor * v[1], factor * v[2], factor * v[3]);
-    else *sum = v;
 }
 
 template <class S>
@@ -639,9 +665,24 @@ struct DxDone : NothingAhead {
                 g.part_out(room, a.parts + (size_t)it.part * (S::TM * S::TN), w.qn - it.tn * S::TN);
                 return 0;
             }
+        int slot[row_regs<S>()], target[row_regs<S>()];
+        float rest[row_regs<S>()];
+#pragma unroll
+        for (int k = 0; k < row_regs<S>(); ++k) {
+            const int row = row_held<S>(g, it, k);
+            const bool on = a.final && row < w.qn;
+            slot[k] = on ? a.rows[row] : 0;
+            target[k] = on ? a.target[row] : 0;
+            rest[k] = on ? a.target_rest[row] : 0.f;
+        }
         const int m0 = it.tm * S::TM, n0 = it.tn * S::TN;
         g.template rows_out<4>(room, [&](int i, int j, int r) __attribute__((always_inline)) { return g.sum(i, j, r); },
-                               [&](int n, int m, const i32x4& v) __attribute__((always_inline)) { put_dx<!S::RING>(a, factor, w.qn, n0 + n, m0 + m, __builtin_bit_cast(f32x4, v)); });
+                               [&](int n, int m, const i32x4& v, int j) __attribute__((always_inline)) {
+                                   const int from = n - g.wn * (S::BN * 16) - j / 4 * 64;       // lane that holds the row's values
+                                   const int s = __shfl(slot[j / 4], from), t = __shfl(target[j / 4], from);
+                                   const float r = __shfl(rest[j / 4], from);
+                                   if (n0 + n < w.qn && m0 + m < a.hidden) put_dx(a, factor, n0 + n, m0 + m, __builtin_bit_cast(f32x4, v), s, t, r);
+                               });
         return n0 + S::TN <= w.qn && m0 + S::TM <= a.hidden ? row_stores<S, 4>() : 0;
     }
 };
@@ -659,22 +700,12 @@ __global__ void __launch_bounds__(256) loss_dx_parts_kernel(GradArgs a) {
     const Work w = dx_work<S>(a);
     const float factor = *a.factor;
     join_parts<S>(w, a.parts, [&](int tm, int tn, int n, int m, const f32x4& v) __attribute__((always_inline)) {
-        put_dx<!S::RING>(a, factor, w.qn, tn * S::TN + n, tm * S::TM + m, v);
+        const int row = tn * S::TN + n, col = tm * S::TM + m;
+        if (row < w.qn && col < a.hidden) put_dx(a, factor, row, col, v, a.rows[row], a.target[row], a.final ? a.target_rest[row] : 0.f);
     });
 }
 
 // ------------------------------------------------------------------------------------------
-// Tiles.  `Slots32` .. `Slots128` serve calls of few slots: four wavefronts side by side along the words (or columns).
-template <bool MP, bool MQ> using Wide = GemmShape<2, 2, 8, 8, MP, MQ>;
-template <bool MP, bool MQ> using Half = GemmShape<2, 2, 4, 4, MP, MQ>;
-template <bool MP, bool MQ> using Slots128 = GemmShape<4, 1, 4, 8, MP, MQ>;
-template <bool MP, bool MQ> using Slots64 = GemmShape<4, 1, 4, 4, MP, MQ>;
-template <bool MP, bool MQ> using Slots32 = GemmShape<4, 1, 4, 2, MP, MQ>;
-// the same with tiles of 128 words
-using Slots128Low = GemmShape<4, 1, 2, 8, false, false>;
-using Slots64Low = GemmShape<4, 1, 2, 4, false, false>;
-using Slots32Low = GemmShape<4, 1, 2, 2, false, false>;
-
 static int slot_tile(int n_q) { return n_q <= 32 ? 32 : n_q <= 64 ? 64 : n_q <= 128 ? 128 : 256; }
 
 // Words to a piece: D of a piece takes up to kPieceBytes, and dX's partial sums (8 bytes of traffic a piece, slot and column) stay below 3 % of the
@@ -691,7 +722,7 @@ struct LossLayout {
     size_t off_count, off_factor, off_slot_target, off_block_count, off_block_max, off_rows, off_target, off_row_lse, off_row_weight, off_target_rest, off_parts;
     size_t off_part, off_target_logit, fwd_bytes;                 // forward
     size_t off_rows_x, off_d, off_dx_sum, bwd_bytes;              // backward
-    int blocks, tile, word_tile, word_tiles, pitch_rows, piece, pieces, twice;
+    int blocks, tile, word_tile, word_tiles, pitch_rows, piece, pieces;
 };
 
 static LossLayout loss_layout(const wlb_vocab_desc& d) {
@@ -726,10 +757,9 @@ static LossLayout loss_layout(const wlb_vocab_desc& d) {
     L.off_target_logit = take(4 * n_q);
     L.fwd_bytes = at;
     at = common;
-    // up to 32 slots fill half of a step of dE's sum: D's rows have room for what bf16 leaves out of them, and dE is exact but for its own rounding
-    L.twice = 2 * n_q <= (size_t)kStepK;
-    L.off_rows_x = take(2 * n_q * h * (L.twice ? 2 : 1));
-    L.off_d = take(2 * n_q * (size_t)L.piece * (L.twice ? 2 : 1));
+    const size_t rows = n_q + std::min(n_q, (size_t)kExactRows);         // how many slots have a target is known on the device
+    L.off_rows_x = take(2 * rows * h);
+    L.off_d = take(2 * rows * (size_t)L.piece);
     L.off_dx_sum = take(L.pieces > 1 ? 4 * n_q * h : 0);
     L.bwd_bytes = at;
     return L;
@@ -866,9 +896,9 @@ extern "C" wlb_status wlb_loss_bwd(const wlb_vocab_desc* desc, const void* x, co
     a.table = (const __bf16*)table; a.rows_x = (__bf16*)(ws + L.off_rows_x); a.d = (__bf16*)(ws + L.off_d);
     a.dx = (__bf16*)dx; a.dtable = (__bf16*)dtable; a.dx_sum = (float*)(ws + L.off_dx_sum);
     a.rows = r.rows; a.target = r.target; a.count = r.count; a.row_lse = r.row_lse; a.row_weight = r.row_weight; a.factor = r.factor;
-    a.target_rest = (float*)(ws + L.off_target_rest); a.twice = L.twice;
+    a.target_rest = (float*)(ws + L.off_target_rest);
     a.vocab = d.vocab; a.hidden = d.hidden; a.n_q = d.n_q; a.pitch = L.piece; a.c2 = d.scale * kLog2e;
-    loss_gather_kernel<<<(d.n_q + 3) / 4, 256, 0, stream>>>((const uint4*)x, (uint4*)a.rows_x, (uint4*)dx, a.rows, r.slot_target, a.count, d.n_q, d.hidden / 8, L.twice);
+    loss_gather_kernel<<<(d.n_q + 3) / 4, 256, 0, stream>>>((const uint4*)x, (uint4*)a.rows_x, (uint4*)dx, a.rows, r.slot_target, a.count, d.n_q, d.hidden / 8);
     a.parts = (float*)(ws + L.off_parts);
     const bool low = L.word_tile < kWordTile;
     for (int p = 0; p < L.pieces; ++p) {
