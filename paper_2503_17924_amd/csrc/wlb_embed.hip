@@ -306,6 +306,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(SortArgs a, 
 // piece, last_part: the one that goes on in the next), which embed_join_kernel adds up in order.
 // Bound by memory: every row of dx once, every row of dtable once (overwriting) or the present ones twice (adding).
 constexpr int kSumUnroll = 8, kFillRows = 16;
+constexpr int kFillMost = 1 << 20;              // workgroups that fill, at most
 
 struct SumArgs {
     const int32_t *word, *slot;
@@ -355,18 +356,20 @@ __device__ __forceinline__ void put_part(const SumArgs& a, int piece, int last, 
 __global__ void __launch_bounds__(256) embed_sum_kernel(SumArgs a) {
     const int wave = uniform((int)threadIdx.x >> 6), lane = threadIdx.x & 63, n = a.n_q;
     if ((int)blockIdx.x >= a.sum_blocks) {
-        const int row0 = (((int)blockIdx.x - a.sum_blocks) * 4 + wave) * kFillRows, row = row0 + lane;
-        bool absent = false;
-        if (lane < kFillRows && row < a.vocab) {
-            const int at = lower_bound(a.word, n, row);
-            absent = at >= n || a.word[at] != row;
-        }
-        unsigned long long todo = __ballot(absent);
-        while (todo) {
-            const int r = __ffsll(todo) - 1;
-            todo &= todo - 1;
-            uint4* to = a.dtable + (size_t)(row0 + r) * a.chunks;
-            for (int c = lane; c < a.chunks; c += 64) to[c] = uint4{0, 0, 0, 0};
+        for (int row0 = (((int)blockIdx.x - a.sum_blocks) * 4 + wave) * kFillRows; row0 < a.vocab; row0 += kFillMost * 4 * kFillRows) {
+            const int row = row0 + lane;
+            bool absent = false;
+            if (lane < kFillRows && row < a.vocab) {
+                const int at = lower_bound(a.word, n, row);
+                absent = at >= n || a.word[at] != row;
+            }
+            unsigned long long todo = __ballot(absent);
+            while (todo) {
+                const int r = __ffsll(todo) - 1;
+                todo &= todo - 1;
+                uint4* to = a.dtable + (size_t)(row0 + r) * a.chunks;
+                for (int c = lane; c < a.chunks; c += 64) to[c] = uint4{0, 0, 0, 0};
+            }
         }
         return;
     }
@@ -514,8 +517,12 @@ extern "C" wlb_status wlb_embed_fwd(const wlb_vocab_desc* desc, const int32_t* t
     int lanes_log2 = 0;
     while ((1 << lanes_log2) < chunks && lanes_log2 < 8) ++lanes_log2;
     const int rows = (256 >> lanes_log2) * kLookupRows;
-    embed_fwd_kernel<<<(desc->n_q + rows - 1) / rows, 256, 0, (hipStream_t)stream>>>(tokens, q_idx, (const uint4*)table, (uint4*)x, desc->n_q, desc->t_kv,
-                                                                                    desc->vocab, chunks, lanes_log2, desc->scale);
+    const int most = (int)std::min((1LL << 23) * rows, (long long)desc->n_q);      // slots to a launch, which has fewer than 2^32 threads
+    for (int first = 0; first < desc->n_q; first += most) {
+        const int n = std::min(most, desc->n_q - first);
+        embed_fwd_kernel<<<(n + rows - 1) / rows, 256, 0, (hipStream_t)stream>>>(tokens, q_idx + first, (const uint4*)table, (uint4*)x + (size_t)first * chunks, n,
+                                                                                 desc->t_kv, desc->vocab, chunks, lanes_log2, desc->scale);
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(WLB_ERR_HIP, "lookup launch: %s", hipGetErrorString(e));
     return WLB_OK;
@@ -563,9 +570,9 @@ extern "C" wlb_status wlb_embed_bwd(const wlb_vocab_desc* desc, const int32_t* t
     a.vocab = d.vocab; a.chunks = d.hidden / 8; a.strips = (a.chunks + 63) / 64;
     a.piece = L.piece; a.pieces = L.pieces; a.add = d.flags & WLB_VOCAB_ACCUMULATE; a.scale = d.scale;
     a.sum_blocks = (int)(((long long)a.pieces * a.strips + 3) / 4);
-    const int fill_blocks = a.add ? 0 : (d.vocab + 4 * kFillRows - 1) / (4 * kFillRows);
+    const int fill_blocks = a.add ? 0 : std::min((d.vocab + 4 * kFillRows - 1) / (4 * kFillRows), kFillMost);
     embed_sum_kernel<<<a.sum_blocks + fill_blocks, 256, 0, stream>>>(a);
-    if (a.pieces > 1) embed_join_kernel<<<(unsigned)a.pieces * a.strips, 256, 0, stream>>>(a);
+    if (a.pieces > 1) embed_join_kernel<<<(unsigned)(a.pieces - 1) * a.strips, 256, 0, stream>>>(a);       // nothing goes on behind the last piece
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(WLB_ERR_HIP, "lookup gradient launch: %s", hipGetErrorString(e));
     return WLB_OK;

@@ -419,17 +419,18 @@ __global__ void __launch_bounds__(256) loss_join_kernel(const float2* part, cons
 
 // ------------------------------------------------------------------------------------------
 // Backward.  The labelled rows of x one behind the other (few of them once more, for D's second set of rows), and zeros in dx of the other slots.
+constexpr int kGatherMost = 1 << 20;           // workgroups at most
 __global__ void __launch_bounds__(256) loss_gather_kernel(const uint4* x, uint4* rows_x, uint4* dx, const int32_t* rows, const int32_t* slot_target,
                                                           const int32_t* count, int n_q, int chunks) {
-    const int i = (int)blockIdx.x * 4 + ((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (i >= n_q) return;
-    const int n = *count;
-    const bool row = i < n, none = slot_target[i] < 0;
-    const size_t from = row ? (size_t)rows[i] * chunks : 0;
-    for (int c = lane; c < chunks; c += 64) {
-        if (row) rows_x[(size_t)i * chunks + c] = x[from + c];
-        if (row && n <= kExactRows) rows_x[(size_t)(n + i) * chunks + c] = x[from + c];
-        if (none) dx[(size_t)i * chunks + c] = uint4{0, 0, 0, 0};
+    const int lane = threadIdx.x & 63, n = *count;
+    for (int i = (int)blockIdx.x * 4 + ((int)threadIdx.x >> 6); i < n_q; i += kGatherMost * 4) {
+        const bool row = i < n, none = slot_target[i] < 0;
+        const size_t from = row ? (size_t)rows[i] * chunks : 0;
+        for (int c = lane; c < chunks; c += 64) {
+            if (row) rows_x[(size_t)i * chunks + c] = x[from + c];
+            if (row && n <= kExactRows) rows_x[(size_t)(n + i) * chunks + c] = x[from + c];
+            if (none) dx[(size_t)i * chunks + c] = uint4{0, 0, 0, 0};
+        }
     }
 }
 
@@ -898,7 +899,7 @@ extern "C" wlb_status wlb_loss_bwd(const wlb_vocab_desc* desc, const void* x, co
     a.rows = r.rows; a.target = r.target; a.count = r.count; a.row_lse = r.row_lse; a.row_weight = r.row_weight; a.factor = r.factor;
     a.target_rest = (float*)(ws + L.off_target_rest);
     a.vocab = d.vocab; a.hidden = d.hidden; a.n_q = d.n_q; a.pitch = L.piece; a.c2 = d.scale * kLog2e;
-    loss_gather_kernel<<<(d.n_q + 3) / 4, 256, 0, stream>>>((const uint4*)x, (uint4*)a.rows_x, (uint4*)dx, a.rows, r.slot_target, a.count, d.n_q, d.hidden / 8);
+    loss_gather_kernel<<<std::min((d.n_q + 3) / 4, kGatherMost), 256, 0, stream>>>((const uint4*)x, (uint4*)a.rows_x, (uint4*)dx, a.rows, r.slot_target, a.count, d.n_q, d.hidden / 8);
     a.parts = (float*)(ws + L.off_parts);
     const bool low = L.word_tile < kWordTile;
     for (int p = 0; p < L.pieces; ++p) {
