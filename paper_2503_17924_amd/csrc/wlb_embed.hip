@@ -78,10 +78,12 @@ __global__ void __launch_bounds__(256) embed_fwd_kernel(const int32_t* tokens, c
 //
 // Up to kSearchMost slots: a slot's place is the number of slots that come before it.  Tiles of 256 slots are sorted by comparing all with
 // all, then every slot finds its place among each tile's words by a binary search, on the whole GPU (16408 slots: 18 us in all; one workgroup sorting by
-// digits took 38 us for half as many).  Above that digit by digit, three launches a pass (16408 slots: 45 us in all, nearly the same for twice as many).
+// digits took 38 us for half as many).  The searches grow with the square of the slots.  Above that digit by digit, three launches a pass.  The whole gradient at
+// hidden 64, by search and by digits, us: 16384 slots, 32768 words 29 and 45 (131072 words: 33 and 52), 32768 slots 36 and 49 (42 and 58), 49152 slots 51 and 54 (58
+// and 64), 65536 slots 70 and 59 (72 and 68), 131072 slots 192 and 76 (194 and 92).
 // Up to kDirectMost slots: one launch, in which workgroups of kDirectSlots slots compare them with all (372 slots: 5 us, the three launches 9).
 constexpr int kDirectMost = 1024, kDirectSlots = 64;
-constexpr int kSearchMost = 131072, kSearchTile = 256, kSearchGroup = 16;       // tiles that a workgroup searches
+constexpr int kSearchMost = 53248, kSearchTile = 256, kSearchGroup = 16;       // tiles that a workgroup searches
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kDigitBits = 9;
 constexpr int kSortBlock = 4 * kSortThreads;                    // slots per workgroup of the sort by digits
 

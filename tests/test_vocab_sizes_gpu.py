@@ -1,9 +1,9 @@
-"""The largest sizes of the vocabulary calls: more rows than one launch has threads for."""
+"""Sizes at which the vocabulary calls change what they launch: another sort, more rows than one launch has threads for."""
 import numpy as np
 import pytest
 
 from paper_2503_17924_amd import binding as B
-from test_vocab_gpu import DEV
+from test_vocab_gpu import DEV, Ends
 
 pytestmark = pytest.mark.gpu
 GIB = 1 << 30
@@ -14,6 +14,11 @@ def room(gib):
     torch.cuda.empty_cache()
     if torch.cuda.mem_get_info()[0] < gib * GIB:
         pytest.skip(f"{gib} GiB of device memory")
+
+
+@pytest.mark.parametrize("docs,vocab,hidden", [([53248], 70000, 8), ([53249], 70000, 8), ([53249], 3, 64), ([40000, 30000], 300000, 72), ([100000], 32767, 16)])
+def test_lookup_gradient_around_the_largest_list_that_is_sorted_by_search(docs, vocab, hidden):
+    Ends(61, docs, 1, 0, vocab, hidden, 2.0).check_embed_bwd()
 
 
 def test_lookup_of_more_slots_than_a_launch_has_threads_for():
