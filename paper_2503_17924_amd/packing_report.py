@@ -20,7 +20,8 @@ and the a (picoseconds per token^2) that a least-squares fit of the measured lat
 
 With --vocab N the part of the linear work that this library has, the two ends of the model (lookup of the micro-batch's tokens, loss over N
 words, the gradients of both), is measured on every micro-batch too and stands in the step in addition to b * tokens, which then models the
-layers between; its own linear cost in picoseconds per token is fitted and printed.
+layers between.  Its own linear cost in picoseconds per token is fitted to the windows as they arrived and added to the b that the packers and the model use, so that
+they balance what the step counts; the fit over all micro-batches is printed at the end.
 
 Usage (on the GPU):  python -m paper_2503_17924_amd.packing_report [--iterations 6] [--vocab 32768 [--hidden 1024]]
 """
@@ -51,6 +52,12 @@ def arrival_windows(doc_len, window: int):
                 seqs.append(cur)
                 cur, used = [], 0
     return seqs          # the unfinished tail is left out
+
+
+def per_token_ps(tokens, ms) -> float:
+    """Least squares of milliseconds to a linear cost, in picoseconds per token."""
+    x, y = np.asarray(tokens, dtype=np.float64), np.asarray(ms, dtype=np.float64)
+    return float((x * y).sum() / (x * x).sum()) * 1e9
 
 
 def time_vocabulary(torch, B, docs, vocab, hidden, reps=2, seed=0):
@@ -128,11 +135,17 @@ def main():
         _, lens, mb, _, _ = state["packer"].step(ids, cur)
         return [[int(x) for x in lens[mb == j]] for j in range(n_mb)]
 
+    cost_b = COST_B
+    if args.vocab:
+        windows = seqs[:n_mb]
+        cost_b += round(per_token_ps([sum(m) for m in windows], [vocabulary_ms(m) for m in windows]))
+        print(f"the packers balance b={cost_b} ps: {COST_B} for the layers, {cost_b - COST_B} measured for lookup, loss and gradients")
+
     packers = [
         ("fixed (arrival order)", fixed, lambda: {}),
-        ("greedy, L_max = window", greedy, lambda: {"packer": B.Packer(n_mb, WINDOW, COST_A, COST_B), "next_id": 0}),
+        ("greedy, L_max = window", greedy, lambda: {"packer": B.Packer(n_mb, WINDOW, COST_A, cost_b), "next_id": 0}),
         ("greedy, L_max = 1.5 window, queues 64K/96K", greedy,
-         lambda: {"packer": B.Packer(n_mb, WINDOW * 3 // 2, COST_A, COST_B, [WINDOW // 2, WINDOW * 3 // 4]), "next_id": 0}),
+         lambda: {"packer": B.Packer(n_mb, WINDOW * 3 // 2, COST_A, cost_b, [WINDOW // 2, WINDOW * 3 // 4]), "next_id": 0}),
     ]
     imb = lambda xs: max(xs) / (sum(xs) / len(xs))
     fit_x, fit_y = [], []
@@ -144,7 +157,7 @@ def main():
             mbs = build(state, it, cur)
             if any(len(m) == 0 for m in mbs):
                 continue          # the queues are still filling: not every micro-batch has work yet
-            model = [sum(COST_A * x * x + COST_B * x for x in m) for m in mbs]
+            model = [sum(COST_A * x * x + cost_b * x for x in m) for m in mbs]
             att = [attention_ms(m) for m in mbs]
             step = [a_ms + COST_B * sum(m) * 1e-9 + vocabulary_ms(m) for a_ms, m in zip(att, mbs)]
             rows.append((imb(model), imb(att), imb(step), max(att), max(step), float(sum(sum(m) for m in mbs))))
@@ -161,9 +174,10 @@ def main():
           f"(the packers used a = {COST_A})")
     if args.vocab:
         x, y = np.array([sum(m) for m in vocab_cache], dtype=np.float64), np.array(list(vocab_cache.values()))
-        off = np.abs(y - x * (x * y).sum() / (x * x).sum()) / y
-        print(f"lookup, loss and gradients, {args.vocab} words, hidden {hidden}: {(x * y).sum() / (x * x).sum() * 1e9:.0f} ps per token "
-              f"(least squares; worst of {len(y)} micro-batches {off.max() * 100:.1f} % off), {100 * (x * y).sum() / (x * x).sum() * 1e9 / COST_B:.1f} % of the b that the packers used")
+        ps = per_token_ps(x, y)
+        off = np.abs(y - x * ps * 1e-9) / y
+        print(f"lookup, loss and gradients, {args.vocab} words, hidden {hidden}: {ps:.0f} ps per token "
+              f"(least squares; worst of {len(y)} micro-batches {off.max() * 100:.1f} % off; the packers used {cost_b - COST_B})")
 
 
 if __name__ == "__main__":
