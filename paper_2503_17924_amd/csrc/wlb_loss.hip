@@ -455,6 +455,12 @@ __device__ __forceinline__ Work d_work(const GradArgs& a) {
     return Work::make<S>(a.table + (size_t)a.piece0 * a.hidden, a.hidden, a.piece_n, a.rows_x, a.hidden, ld_const(a.count), nullptr, a.hidden, a.workgroups, kNever);
 }
 
+// What bf16 leaves out of d: nothing, beside a value that is not finite.
+__device__ __forceinline__ float left_out(float d) {
+    const float rest = d - (float)(__bf16)d;
+    return __builtin_isfinite(rest) ? rest : 0.f;
+}
+
 template <class S>
 struct DDone {
     const GradArgs& a;
@@ -517,14 +523,14 @@ struct DDone {
                     if (!mine) return;
                     const float d = weight[j] * (share(l, j) - 1.f);
                     set(t + (g.lane / 16) * 4, d);
-                    a.target_rest[n0 + g.wn * (S::BN * 16) + j * 16 + g.lane % 16] = d - (float)(__bf16)d;
+                    a.target_rest[n0 + g.wn * (S::BN * 16) + j * 16 + g.lane % 16] = left_out(d);
                 });
             if (S::RING || w.qn > kExactRows) return;
             g.template rows_out<2>(
                 room,
                 [&](int i, int j, int r) __attribute__((always_inline)) {
                     const float p = share(g.sum(i, j, r), j), d = weight[j] * (target[j] == i * 16 + r ? p - 1.f : p);
-                    return edge && first + i * 16 + r >= a.piece_n ? 0.f : d - (float)(__bf16)d;
+                    return edge && first + i * 16 + r >= a.piece_n ? 0.f : left_out(d);
                 },
                 [&](int n, int m, const i32x4& v, int) __attribute__((always_inline)) {
                     if (n0 + n < w.qn) *reinterpret_cast<i32x4*>(a.d + (size_t)(w.qn + n0 + n) * a.pitch + m0 + m) = v;
@@ -570,7 +576,7 @@ __global__ void __launch_bounds__(256) loss_d_parts_kernel(GradArgs a) {
         for (int k = 0; k < 4; ++k) {
             const float p = word + k < a.piece_n ? fast_exp2(__builtin_fmaf(l[k], a.c2, -lse2)) : 0.f;
             d[k] = weight * (t == k ? p - 1.f : p);
-            if (t == k) a.target_rest[row] = d[k] - (float)(__bf16)d[k];
+            if (t == k) a.target_rest[row] = left_out(d[k]);
         }
         *reinterpret_cast<bf16x4*>(a.d + (size_t)row * a.pitch + word) = pack4(d[0], d[1], d[2], d[3]);
     });

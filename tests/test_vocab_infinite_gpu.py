@@ -69,3 +69,25 @@ def test_logits_beyond_the_largest_float(slots, vocab, hidden):
     dx, dt = e.loss_bwd(lse)
     assert torch.isfinite(dx[dev(~up)]).all() and torch.isfinite(dt[others]).all()
     assert torch.isnan(dx[dev(up & has)]).all() and torch.isnan(dt[far]).all()
+
+
+@pytest.mark.parametrize("slots,vocab,hidden", [(20, 300, 64), (25, 70001, 136), (200, 1000, 64), (1500, 777, 1032)])
+def test_an_infinite_gradient_of_one_loss(slots, vocab, hidden):
+    """Few slots with a target, one of them with an infinite weight: the table's gradient is infinite with the sign that the definition gives, not undefined."""
+    import torch
+    e = Ends(32, [slots], 1, 0, vocab, hidden, masked=0.0, logit=1.0)
+    tok = np.full(slots, -1, np.int32)
+    tok[1:18] = np.random.default_rng(4).integers(0, vocab, 17)
+    e.tok, e.tokens = tok, torch.from_numpy(tok).to(DEV)
+    e.target = plain.targets(tok, e.q_idx, e.cu, vocab)
+    e.x = torch.randn(slots, hidden, device=DEV, generator=torch.Generator(DEV).manual_seed(3)).bfloat16()
+    e.x[e.x == 0] = 1.0
+    e.d_loss = torch.rand(slots, device=DEV)
+    e.d_loss[3] = float("inf")
+    dx, dt = e.loss_bwd(e.loss()[1])
+    sign = torch.ones(vocab, 1, device=DEV)
+    sign[e.target[3]] = -1
+    assert torch.equal(dt.float(), sign * e.x[3].float().sign() * float("inf"))
+    finite = torch.ones(slots, dtype=torch.bool, device=DEV)
+    finite[3] = False
+    assert torch.isfinite(dx[finite]).all() and not torch.isfinite(dx[3]).any()
