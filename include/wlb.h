@@ -389,10 +389,10 @@ wlb_status wlb_attn_bwd(const wlb_attn_desc* desc, const void* q, const void* k,
  *           backward computes them again for one piece of the vocabulary at a time.
  *
  * The gradients are those of sum_i d_loss[i] * loss[i] and of sum <dx, x>; dtable is THIS rank's partial sum (as dK / dV of
- * the attention).  Sums are held in 32 bits and in an order that the sizes alone decide: deterministic, no
- * floating-point atomics.  dx, dtable and x are rounded to bf16 once.  The logits' gradient, relative to the largest
- * |d_loss|, enters its two matrix products in bf16.  What that leaves out at the targets is added to dx; where up to 32 slots have a
- * target, whose roundings find little to average out with, all that it leaves out is added to dtable.
+ * the attention).  Sums are held in 32 bits and in an order that follows from the sizes, the slots' words or how many slots have a
+ * target, and the device's compute units: the same call on the same values gives the same bits; no floating-point atomics.  dx, dtable and x are rounded to bf16 once.  The logits' gradient, relative to the largest
+ * |d_loss|, enters its two matrix products in bf16 (up to 2^-8 of each term of their sums).  What that leaves out at the targets is
+ * added to dx; where up to 32 slots have a target, whose roundings find little to average out with, all that it leaves out is added to dtable.
  * What a call writes overlaps neither what it reads nor its workspace.
  */
 typedef struct {

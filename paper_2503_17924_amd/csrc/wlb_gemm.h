@@ -6,7 +6,7 @@
 // contiguous (rows of m or n: "K") or with m or n contiguous (rows of k: "M"); the second kind is read from LDS with transpose reads, so
 // no operand is ever written transposed.  Wide tiles (256 x 256) take one workgroup to a compute unit and one wavefront to a SIMD: a wavefront's
 // 128 x 128 part needs 16 KiB of LDS reads for 64 MFMAs, two thirds of what 8 wavefronts of 128 x 64 would read.  They are bound by the MFMA rate at
-// the clock that the power limit leaves (1.5 - 1.8 GHz).  Narrow tiles (few slots) are bound by the table's bytes.
+// the clock that the power limit leaves (16385 slots, 65536 words, hidden 4096: MFMAs busy 70 % of the cycles at 1.83 GHz; in the library's product 80 % at 1.66).  Narrow tiles (few slots) are bound by the table's bytes.
 #pragma once
 #include <type_traits>
 

@@ -7,8 +7,9 @@
 //   backward  D = w (exp(c l - lse) - [v = target]) with w = d_loss / G, G the largest |d_loss|, in bf16, for one piece of the vocabulary at a
 //             time; then dE = c G D^T X for the piece's rows and dX += D E over the pieces, in fp32; dX is scaled by c G at the end.
 //             G keeps the factor that most training steps have in common (1 / tokens) out of the rounding of D.  What bf16 leaves out of D at a row's
-//             target, the largest of its entries, is added to dX in fp32.  In dE the roundings of many rows average out; up to kExactRows rows, which fill
-//             half of a step of its sum, D has a second set of rows with all that bf16 leaves out of the first.
+//             target, the largest of its entries, is added to dX in fp32.  dE keeps D's roundings, up to 2^-8 of each term of its sums: as much as its own rounding
+//             where one row makes up the sum, less where many rows' roundings average out.  Up to kExactRows rows, which fill half of a step of its
+//             sum, D has a second set of rows with all that bf16 leaves out of the first, and dE is exact but for its own rounding.
 // Slots without a target are left out of everything: the others are listed in order (rows), and products run over that list.
 // Bound by the matrix products: 2 n V H operations forward, 6 n V H backward, where 64 slots or more share the table's
 // rows; by the table's bytes below that.
@@ -715,8 +716,8 @@ __global__ void __launch_bounds__(256) loss_dx_parts_kernel(GradArgs a) {
 // ------------------------------------------------------------------------------------------
 static int slot_tile(int n_q) { return n_q <= 32 ? 32 : n_q <= 64 ? 64 : n_q <= 128 ? 128 : 256; }
 
-// Words to a piece: D of a piece takes up to kPieceBytes, and dX's partial sums (8 bytes of traffic a piece, slot and column) stay below 3 % of the
-// time of the products where a piece has kPieceMin words.
+// Words to a piece: D of a piece takes up to kPieceBytes, but a piece has kPieceMin words at least (above 16384 slots that is more: 4 GiB at 131072 slots), with
+// which dX's partial sums (8 bytes of traffic a piece, slot and column) stay below 3 % of the time of the products.
 constexpr size_t kPieceBytes = 512u << 20;
 constexpr int kPieceMin = 16384;
 
