@@ -86,3 +86,45 @@ def test_rows_whose_gradient_is_their_target_alone(slots, vocab, hidden):
     e.x = (sure * row / (row @ row) + noise).bfloat16()
     e.d_loss.fill_(1.0)
     check(e)
+
+
+def test_graph_whose_replays_have_few_many_and_no_targets():
+    """What a captured call launches does not depend on how many slots have a target."""
+    import torch
+    e = Ends(26, [700], 1, 0, 3000, 136, masked=0.0)
+    full, weight = e.tok.copy(), torch.rand(e.n_q, device=DEV)
+    e.x.nan_to_num_(1.0)
+    e.d_loss.copy_(weight)
+    ends = B.Vocabulary(e.q_idx, e.cu, e.vocab, e.hidden, logit_scale=0.8)
+    f32, bf = torch.float32, torch.bfloat16
+    loss, lse = torch.empty(e.n_q, dtype=f32, device=DEV), torch.empty(e.n_q, dtype=f32, device=DEV)
+    dx, dt = torch.empty(e.n_q, e.hidden, dtype=bf, device=DEV), torch.empty(e.vocab, e.hidden, dtype=bf, device=DEV)
+
+    def step():
+        ends.loss(e.x, e.table, e.tokens, loss, lse)
+        ends.loss_backward(e.x, e.table, e.tokens, lse, e.d_loss, dx, dt)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for labelled in (5, 699, 0, 32, 33, 128, 1):
+        tok = np.full_like(full, -1)
+        at = np.random.default_rng(labelled).permutation(699)[:labelled] + 1
+        tok[at] = full[at]
+        e.tokens.copy_(torch.from_numpy(tok))
+        for t in (loss, lse, dx, dt):
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        target = plain.targets(tok, e.q_idx, e.cu, e.vocab)
+        has = np.flatnonzero(target >= 0)
+        rows = torch.from_numpy(has).to(DEV)
+        want = plain.loss_bwd(e.x[rows], e.table, target[has], 0.8, weight[rows])
+        plain.check(f"dx, {labelled}", dx[rows], want[0], want[2])
+        plain.check(f"dtable, {labelled}", dt, want[1], want[3])
+        replayed = [t.clone() for t in (loss, lse, dx, dt)]
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(replayed, (loss, lse, dx, dt))), labelled

@@ -98,3 +98,58 @@ def test_loss_of_more_slots_than_a_launch_has_threads_for():
     assert not loss.any() and not dx.any()
     del x, dx, workspace
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("slots", [20, 200])
+@pytest.mark.parametrize("hidden", [32776, 33024, 65528, 65536])
+def test_widest_rows(slots, hidden):
+    """As many tiles of columns as half of the compute units, one more, and as many as all."""
+    e = Ends(62, [slots], 1, 0, 300, hidden, masked=0.0)
+    e.check_embed()
+    e.check_embed_bwd()
+    e.check_loss()
+
+
+def test_loss_of_the_largest_vocabulary():
+    """2^30 words, four pieces; one slot with a target.  The definition in 64 bits, a part of the words at a time."""
+    import torch
+    room(60)
+    vocab, hidden, part = 2 ** 30, 8, 2 ** 24
+    g = torch.Generator(DEV).manual_seed(7)
+    table = torch.empty(vocab, hidden, dtype=torch.bfloat16, device=DEV)
+    for a in range(0, vocab, part):
+        table[a:a + part] = torch.randn(part, hidden, device=DEV, generator=g).bfloat16()
+    x = torch.randn(2, hidden, device=DEV, generator=g).bfloat16()
+    target = vocab - 3
+    tokens = torch.tensor([5, target], dtype=torch.int32, device=DEV)
+    q_idx, cu = torch.arange(2, dtype=torch.int32, device=DEV), torch.tensor([0, 2], dtype=torch.int32, device=DEV)
+    desc = B.vocab_desc(2, 2, 1, vocab, hidden)
+    workspace = torch.empty(max(B.wlb_vocab_workspace_size(desc)[1:]), dtype=torch.uint8, device=DEV)
+    loss, lse = torch.empty(2, device=DEV), torch.empty(2, device=DEV)
+    B.wlb_loss_fwd(desc, x, table, tokens, q_idx, cu, loss, lse, workspace)
+    weight = torch.tensor([0.75, float("nan")], device=DEV)
+    dx, dtable = torch.full_like(x, float("nan")), torch.empty_like(table)
+    B.wlb_loss_bwd(desc, x, table, tokens, q_idx, cu, lse, weight, dx, dtable, workspace)
+    row = x[0].double()
+    sums = torch.stack([torch.exp((table[a:a + part].double() * row).sum(1)).sum() for a in range(0, vocab, part)])
+    true = torch.log(sums.sum())
+    own = float(table[target].double() @ row)
+    # a logit is off by its eight products, a part's sum by up to 128 terms in a row and the lse by the parts that a thread adds up, 2^16
+    off = (2 ** 16 + 256) * 2.0 ** -24
+    assert abs(float(lse[0]) - float(true)) <= off and abs(float(loss[0]) - (float(true) - own)) <= off + 1e-5
+    assert float(loss[1]) == 0 and float(lse[1]) == -float("inf") and not dx[1].any()
+    want_dx, size = torch.zeros(hidden, dtype=torch.float64, device=DEV), torch.zeros(hidden, dtype=torch.float64, device=DEV)
+    for a in range(0, vocab, part):
+        e = table[a:a + part].double()
+        d = 0.75 * torch.exp((e * row).sum(1) - true)
+        size += (d[:, None] * e.abs()).sum(0)
+        if a <= target < a + part:
+            d[target - a] -= 0.75
+        want_dx += (d[:, None] * e).sum(0)
+        want = d[:, None] * row
+        # D and what bf16 leaves out of it: 2^-16; the probability's error and the lse's; the output's rounding
+        assert ((dtable[a:a + part].double() - want).abs() <= want.abs() * (2.0 ** -8 + 2.0 ** -15 + 2 * off)).all(), a
+    # D in bf16 but for the target; sums of up to 2^16 products of 32 words in a row
+    assert ((dx[0].double() - want_dx).abs() <= 2.0 ** -8 * want_dx.abs() + (2.0 ** -8 + 3 * off) * size).all()
+    del table, dtable, workspace
+    torch.cuda.empty_cache()
