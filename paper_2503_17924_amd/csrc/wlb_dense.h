@@ -46,6 +46,107 @@ __device__ __forceinline__ float rest_of(float v) {
     return __builtin_isfinite(rest) ? rest : 0.f;
 }
 
+// ------------------------------------------------------------------------------------------
+// Several products in one launch: a workgroup takes its items of one after the other, and those of the next product begin with the workgroups that the last one
+// left without any, so that three products which each leave part of the chip idle share it.  None of them is divided along k but the last one's tiles
+// past whole rounds (or, of few slots, the first).
+struct GroupArgs {
+    ProductArgs a[3];                // the first of kinds MK, if there is one (its qn is 0 otherwise), then those of kinds MM
+    int n;
+    int turn[3];                     // workgroups of an XCD by which a product's first one is moved
+};
+
+// A group of whole tiles, and what it should take: every workgroup of an XCD has its items' time, and the last product's tiles past whole rounds may be divided.
+template <class S>
+long long plan_group(GroupArgs& g, const TileCost& cost) {
+    const int per_cu = S::RING ? 1 : 2, workgroups = wide_workgroups() * per_cu, side = workgroups / kLists;
+    long long load[256] = {};
+    int at = 0;
+    for (int k = 0; k < g.n; ++k) {
+        ProductArgs& a = g.a[k];
+        if (a.qn == 0) continue;
+        const int ntm = (a.pm + S::TM - 1) / S::TM, ntn = (a.qn + S::TN - 1) / S::TN, steps = std::max(2, (a.depth + kStepK - 1) / kStepK);
+        a.grid.ntm = ntm; a.grid.ntn = ntn; a.grid.depth = a.depth; a.grid.workgroups = workgroups;
+        a.grid.whole = ntm * ntn; a.grid.left = 0; a.grid.parts = 1; a.grid.lead = 0;
+        long long part = 0, join = 0;
+        if (k == g.n - 1) {
+            // the tiles of a last round that a quarter of the launch at most would have
+            const int before = at, per = (a.grid.whole + kLists - 1) / kLists, over = (before + per) % side;
+            const int most = std::min(kMaxParts, steps / kWideParts);
+            if (over > 0 && over <= side / 4 && over < per && before + per > side) {
+                const int whole = (per - over) * kLists, left = a.grid.whole - whole, p = left > 0 ? std::min(workgroups / left, most) : 0;
+                if (p >= 2 && (long long)left * p * S::TM * S::TN <= (long long)workgroups * S::TM * S::TN) {
+                    a.grid.whole = whole; a.grid.left = left; a.grid.parts = p;
+                    part = (long long)((steps + p - 1) / p) * cost.step + cost.end;
+                    join = kJoinLaunch + (long long)left * p * cost.join;
+                }
+            }
+        }
+        const int per = (a.grid.whole + kLists - 1) / kLists;
+        g.turn[k] = at % side;
+        for (int i = 0; i < per; ++i) load[(at + i) % side] += (long long)steps * cost.step + cost.end;
+        at += per;
+        if (part) {
+            // An XCD's parts go to the workgroups that are done first of those where a product begins or ends: at equal loads behind the last whole tile, but where
+            // products' steps differ beside the one with fewer (4189 slots, 1544 x 5000, dx's 79 and dW's 66: 145 us, behind dx's tiles 157).
+            const int share = (a.grid.left * a.grid.parts + kLists - 1) / kLists, end = at % side;
+            long long least = 0;
+            for (int c = k + 1; c >= 0; --c) {
+                const int from = c > k ? end : g.a[c].qn ? g.turn[c] : end;
+                long long most = 0;
+                for (int i = 0; i < std::min(share, side); ++i) most = std::max(most, load[(from + i) % side]);
+                if (c > k || most < least) {
+                    least = most;
+                    a.grid.lead = (from - end + side) % side;
+                }
+            }
+            return std::max(*std::max_element(load, load + side), least + part) + join;
+        }
+    }
+    return *std::max_element(load, load + side);
+}
+
+// How the products of a gradient, which wait for nothing of each other, are launched: one after the other, or in one launch of wide, small or tiny tiles; few slots' weights in
+// small tiles, dx in tiles of 128 columns and up to 32, 64 or 128 slots, or in tiny ones.
+enum Group { kApart, kWideGroup, kSmallGroup, kTinyGroup, kFewGroup32, kFewGroup64, kFewGroup128, kFewGroupTiny };
+inline Group plan_gradients(GroupArgs& g) {
+    const bool dx = g.a[0].qn > 0;
+    const int rows = dx ? g.a[0].qn : g.n > 1 ? g.a[1].depth : 0;
+    if (rows == 0 || (dx ? 1 : 0) + g.n - 1 < 2) return kApart;
+    if (rows <= kFewSlots) {
+        // the weights' gradients in tiles of 128 x 128, which are bound by what they write; dx as its product by itself would be
+        const int workgroups = 2 * wide_workgroups(), ntm = (g.a[0].pm + 127) / 128;
+        const bool few = dx && few_slots(true, rows, g.a[0].pm, g.a[0].depth);
+        long long unused = 0;
+        // dx in parts for half of the workgroups, beside which the others begin with the weights' tiles
+        const int half = wide_workgroups();
+        if (few) g.a[0].grid = g.a[0].twin ? joined_grid(ntm, g.a[0].depth, half) : planned_grid(ntm, 1, g.a[0].depth, half, kFewParts, 1);
+        else if (dx) g.a[0].grid = narrow_grid(kTinyCost, g.a[0].pm, rows, g.a[0].depth, unused, g.a[0].twin > 0, half);
+        g.a[0].grid.workgroups = workgroups;
+        int at = dx ? (g.a[0].grid.whole + g.a[0].grid.left * g.a[0].grid.parts + kLists - 1) / kLists : 0;
+        for (int k = 1; k < g.n; ++k) {
+            g.a[k].grid = narrow_grid(kSmallCost, g.a[k].pm, g.a[k].qn, g.a[k].depth, unused);
+            g.a[k].grid.whole += g.a[k].grid.left;
+            g.a[k].grid.left = 0;
+            g.a[k].grid.parts = 1;
+            g.turn[k] = at % (workgroups / kLists);
+            at += (g.a[k].grid.whole + kLists - 1) / kLists;
+        }
+        const int tile = few ? slot_tile(rows) : 0;
+        return tile == 32 ? kFewGroup32 : tile == 64 ? kFewGroup64 : tile == 128 ? kFewGroup128 : kFewGroupTiny;
+    }
+    long long apart = 0;
+    for (int k = 0; k < g.n; ++k)
+        if (g.a[k].qn) apart += best_tiling(g.a[k].pm, g.a[k].qn, g.a[k].depth).cost + kNextLaunch;
+    GroupArgs wide = g, small = g, tiny = g;
+    const long long wide_time = plan_group<Wide<true, true>>(wide, kWideCost), small_time = plan_group<Small<true, true>>(small, kSmallCost), tiny_time = plan_group<Tiny<true, true>>(tiny, kTinyCost);
+    const long long least = std::min({apart, wide_time, small_time, tiny_time});
+    if (apart == least) return kApart;
+    g = wide_time == least ? wide : small_time == least ? small : tiny;
+    return wide_time == least ? kWideGroup : small_time == least ? kSmallGroup : kTinyGroup;
+}
+
+// ------------------------------------------------------------------------------------------
 // Rows of `src` that are listed, one behind the other in `dst` (null: nothing is copied), for up to two tensors; and zeros in the rows of `zero` that are not.
 struct GatherArgs {
     const uint4* src[2];

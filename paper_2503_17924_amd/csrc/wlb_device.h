@@ -71,6 +71,7 @@ __device__ __forceinline__ bf16x4 pack4(float a0, float a1, float a2, float a3) 
 // tells the compiler that a value is the same in every lane (moves it to a scalar register)
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__host__ inline int uniform(int x) { return x; }        // of a work list that the host walks
 
 // Loads through the constant address space: with a wave-uniform address they become scalar
 // loads (counted by lgkmcnt, not vmcnt, so they do not interfere with the asynchronous tile

@@ -70,10 +70,11 @@ constexpr int kBand = 8, kMaxParts = 128;
 constexpr int kEndSteps = 6, kJoinSteps = 4;
 struct GemmGrid {
     int ntm, ntn, depth, workgroups, whole, left, parts;
+    int lead = 0;               // by how many workgroups of an XCD the first part is moved on from the one behind the last whole tile
     // part_steps: a divided tile's part has at least this many steps.  rounds: how many the parts may take; with one, tiles are divided wherever they can be,
     // with more where it pays: 160 tiles of 512 steps on 256 workgroups take 518 steps, in 3 parts each 2 * (171 + 6) and the join's 52.
     GemmGrid() = default;
-    __device__ __forceinline__ GemmGrid(int ntm_, int ntn_, int depth_, int workgroups_, int part_steps, int rounds) : ntm(ntm_), ntn(ntn_), depth(depth_), workgroups(workgroups_) {
+    __host__ __device__ __forceinline__ GemmGrid(int ntm_, int ntn_, int depth_, int workgroups_, int part_steps, int rounds) : ntm(ntm_), ntn(ntn_), depth(depth_), workgroups(workgroups_) {
         const int tiles = ntm * ntn, steps = (depth + kStepK - 1) / kStepK, most = min(kMaxParts, steps / part_steps);
         left = uniform(tiles % workgroups);
         parts = 1;
@@ -87,27 +88,25 @@ struct GemmGrid {
         if (parts == 1) left = 0;
         whole = tiles - left;
     }
-    __device__ __forceinline__ void place(int t, GemmItem& it) const {
+    __host__ __device__ __forceinline__ void place(int t, GemmItem& it) const {
         const int band = t / (kBand * ntm), high = min(kBand, ntn - band * kBand);
         t -= band * kBand * ntm;
         const int tm = t / high;
         it.tm = uniform(tm);            // divisions leave scalars in vector registers
         it.tn = uniform(band * kBand + (t - tm * high));
     }
-    // item `round` of workgroup b; false: there is none
-    __device__ __forceinline__ bool item(int b, int round, GemmItem& it) const {
+    // Item `round` of workgroup b; false: there is none, nor in later rounds.  An XCD's parts follow its whole tiles, a round of them begins with the workgroup `lead` behind
+    // the one after the last whole tile, and each is one workgroup's in one round.
+    __host__ __device__ __forceinline__ bool item(int b, int round, GemmItem& it) const {
         it.tm = it.tn = 0;
         const int x = b % kLists, i = b / kLists, side = workgroups / kLists;
-        const int per = (whole + kLists - 1) / kLists, mine = round * side + i, t = x * per + mine;
+        const int per = (whole + kLists - 1) / kLists, first = x * per, own = max(0, min(per, whole - first)), mine = round * side + i;
         it.k0 = 0; it.depth = depth; it.part = -1;
-        const int rounds = (per + side - 1) / side;
-        if (round < rounds) {
-            if (mine < per && t < whole) { place(t, it); return true; }
-            if (round < rounds - 1 || left == 0) return false;
-            round = rounds;                          // no whole tile in the last round
-        }
+        if (mine < own) { place(first + mine, it); return true; }
+        if (left == 0) return false;
         // every XCD has its share of the parts, however few there are
-        const int share = (left * parts + kLists - 1) / kLists, at = (round - rounds) * side + i, u = x * share + at;
+        const int share = (left * parts + kLists - 1) / kLists, behind = mine - own, turned = behind % side;
+        const int at = behind - turned + (turned >= lead ? turned - lead : turned - lead + side), u = x * share + at;
         if (at >= share || u >= left * parts) return false;
         const int part = u / left, steps = (depth + kStepK - 1) / kStepK;
         place(whole + u - part * left, it);

@@ -222,15 +222,7 @@ void launch_product(Kinds kinds, ProductArgs& a, hipStream_t stream) {
 }
 
 // ------------------------------------------------------------------------------------------
-// Several products in one launch: a workgroup takes its items of one after the other, and those of the next product begin with the workgroups that the last one
-// left without any, so that three products which each leave part of the chip idle share it.  None of them is divided along k but the last one's tiles
-// past whole rounds (or, of few slots, the first).
-struct GroupArgs {
-    ProductArgs a[3];                // the first of kinds MK, if there is one (its qn is 0 otherwise), then those of kinds MM
-    int n;
-    int turn[3];                     // workgroups of an XCD by which a product's first one is moved
-};
-
+// Several products in one launch (GroupArgs).
 // Few slots: two workgroups to a compute unit, as of the small tiles that run beside them.
 template <int BN> using FewBeside = GemmShape<4, 1, 2, BN, true, false, kDivSmall>;
 
@@ -253,40 +245,6 @@ __global__ void __launch_bounds__(256, MM::PER_CU < MK::PER_CU ? MM::PER_CU : MK
     }
 }
 
-// A group of whole tiles, and what it should take: every workgroup of an XCD has its items' time, and the last product's tiles past whole rounds may be divided.
-template <class S>
-static long long plan_group(GroupArgs& g, const TileCost& cost) {
-    const int per_cu = S::RING ? 1 : 2, workgroups = wide_workgroups() * per_cu, side = workgroups / kLists;
-    long long load[256] = {};
-    int at = 0;
-    for (int k = 0; k < g.n; ++k) {
-        ProductArgs& a = g.a[k];
-        if (a.qn == 0) continue;
-        const int ntm = (a.pm + S::TM - 1) / S::TM, ntn = (a.qn + S::TN - 1) / S::TN, steps = std::max(2, (a.depth + kStepK - 1) / kStepK);
-        a.grid.ntm = ntm; a.grid.ntn = ntn; a.grid.depth = a.depth; a.grid.workgroups = workgroups;
-        a.grid.whole = ntm * ntn; a.grid.left = 0; a.grid.parts = 1;
-        long long divided = 0;
-        if (k == g.n - 1) {
-            // the tiles of a last round that a quarter of the launch at most would have
-            const int before = at, per = (a.grid.whole + kLists - 1) / kLists, over = (before + per) % side;
-            const int most = std::min(kMaxParts, steps / kWideParts);
-            if (over > 0 && over <= side / 4 && over < per && before + per > side) {
-                const int whole = (per - over) * kLists, left = a.grid.whole - whole, p = left > 0 ? std::min(workgroups / left, most) : 0;
-                if (p >= 2 && (long long)left * p * S::TM * S::TN <= (long long)workgroups * S::TM * S::TN) {
-                    a.grid.whole = whole; a.grid.left = left; a.grid.parts = p;
-                    divided = (long long)(steps + p - 1) / p * cost.step + cost.end + kJoinLaunch + (long long)left * p * cost.join;
-                }
-            }
-        }
-        const int per = (a.grid.whole + kLists - 1) / kLists;
-        g.turn[k] = at % side;
-        for (int i = 0; i < per; ++i) load[(at + i) % side] += (long long)steps * cost.step + cost.end;
-        at += per;
-        if (divided) return *std::max_element(load, load + side) + divided;
-    }
-    return *std::max_element(load, load + side);
-}
-
 template <class S>
 static void join_last(const ProductArgs& a, hipStream_t stream) {
     if (a.grid.left) product_join_kernel<S><<<join_grid<S>(a.grid), 256, 0, stream>>>(a);
@@ -299,61 +257,43 @@ void launch_gradients(ProductArgs* dx, ProductArgs* const* dw, int n_dw, hipStre
     for (int k = 0; k < n_dw; ++k) g.a[g.n++] = *dw[k];
     for (int k = 0; k < g.n; ++k)
         if (!g.a[k].to) g.a[k].out_limit = g.a[k].twin ? g.a[k].twin : g.a[k].qn;
-    const int rows = dx ? dx->qn : n_dw ? dw[0]->depth : 0;
-    if (rows == 0 || (dx ? 1 : 0) + n_dw < 2) {
+    auto launch = [&](auto first, auto others) {
+        group_kernel<decltype(first), decltype(others)><<<g.a[g.n - 1].grid.workgroups, 256, 0, stream>>>(g);
+    };
+    switch (plan_gradients(g)) {
+    case kApart:
         if (dx) launch_product(Kinds::MK, *dx, stream);
         for (int k = 0; k < n_dw; ++k) launch_product(Kinds::MM, *dw[k], stream);
-        return;
-    }
-    if (rows <= kFewSlots) {
-        // the weights' gradients in tiles of 128 x 128, which are bound by what they write; dx as its product by itself would be
-        const int workgroups = 2 * wide_workgroups(), ntm = (g.a[0].pm + 127) / 128;
-        const bool few = dx && few_slots(true, rows, g.a[0].pm, g.a[0].depth);
-        long long unused = 0;
-        // dx in parts for half of the workgroups, beside which the others begin with the weights' tiles
-        const int half = n_dw ? wide_workgroups() : workgroups;
-        if (few) g.a[0].grid = g.a[0].twin ? joined_grid(ntm, g.a[0].depth, half) : planned_grid(ntm, 1, g.a[0].depth, half, kFewParts, 1);
-        else if (dx) g.a[0].grid = narrow_grid(kTinyCost, g.a[0].pm, rows, g.a[0].depth, unused, g.a[0].twin > 0, half);
-        g.a[0].grid.workgroups = workgroups;
-        int at = dx ? (g.a[0].grid.whole + g.a[0].grid.left * g.a[0].grid.parts + kLists - 1) / kLists : 0;
-        for (int k = 1; k < g.n; ++k) {
-            g.a[k].grid = narrow_grid(kSmallCost, g.a[k].pm, g.a[k].qn, g.a[k].depth, unused);
-            g.a[k].grid.whole += g.a[k].grid.left;
-            g.a[k].grid.left = 0;
-            g.a[k].grid.parts = 1;
-            g.turn[k] = at % (workgroups / kLists);
-            at += (g.a[k].grid.whole + kLists - 1) / kLists;
-        }
-        auto launch = [&](auto s) {
-            using S = decltype(s);
-            group_kernel<S, Small<true, true>><<<workgroups, 256, 0, stream>>>(g);
-            if (dx) join_last<S>(g.a[0], stream);
-        };
-        const int tile = few ? slot_tile(rows) : 256;
-        if (tile == 32) launch(FewBeside<2>{});
-        else if (tile == 64) launch(FewBeside<4>{});
-        else if (tile == 128) launch(FewBeside<8>{});
-        else launch(Tiny<true, false>{});
-        return;
-    }
-    long long apart = 0;
-    for (int k = 0; k < g.n; ++k)
-        if (g.a[k].qn) apart += best_tiling(g.a[k].pm, g.a[k].qn, g.a[k].depth).cost + kNextLaunch;
-    GroupArgs small = g, tiny = g;
-    const long long wide_time = plan_group<Wide<true, true>>(g, kWideCost), small_time = plan_group<Small<true, true>>(small, kSmallCost), tiny_time = plan_group<Tiny<true, true>>(tiny, kTinyCost);
-    const long long least = std::min({apart, wide_time, small_time, tiny_time});
-    if (apart == least) {
-        if (dx) launch_product(Kinds::MK, *dx, stream);
-        for (int k = 0; k < n_dw; ++k) launch_product(Kinds::MM, *dw[k], stream);
-    } else if (wide_time == least) {
-        group_kernel<Wide<true, false>, Wide<true, true>><<<wide_workgroups(), 256, 0, stream>>>(g);
+        break;
+    case kWideGroup:
+        launch(Wide<true, false>{}, Wide<true, true>{});
         join_last<Wide<true, true>>(g.a[g.n - 1], stream);
-    } else if (small_time == least) {
-        group_kernel<Small<true, false>, Small<true, true>><<<2 * wide_workgroups(), 256, 0, stream>>>(small);
-        join_last<Small<true, true>>(small.a[small.n - 1], stream);
-    } else {
-        group_kernel<Tiny<true, false>, Tiny<true, true>><<<2 * wide_workgroups(), 256, 0, stream>>>(tiny);
-        join_last<Tiny<true, true>>(tiny.a[tiny.n - 1], stream);
+        break;
+    case kSmallGroup:
+        launch(Small<true, false>{}, Small<true, true>{});
+        join_last<Small<true, true>>(g.a[g.n - 1], stream);
+        break;
+    case kTinyGroup:
+        launch(Tiny<true, false>{}, Tiny<true, true>{});
+        join_last<Tiny<true, true>>(g.a[g.n - 1], stream);
+        break;
+    // of few slots dx may be divided, beside the weights' whole tiles
+    case kFewGroup32:
+        launch(FewBeside<2>{}, Small<true, true>{});
+        join_last<FewBeside<2>>(g.a[0], stream);
+        break;
+    case kFewGroup64:
+        launch(FewBeside<4>{}, Small<true, true>{});
+        join_last<FewBeside<4>>(g.a[0], stream);
+        break;
+    case kFewGroup128:
+        launch(FewBeside<8>{}, Small<true, true>{});
+        join_last<FewBeside<8>>(g.a[0], stream);
+        break;
+    case kFewGroupTiny:
+        launch(Tiny<true, false>{}, Small<true, true>{});
+        join_last<Tiny<true, false>>(g.a[0], stream);
+        break;
     }
 }
 

@@ -1,0 +1,149 @@
+// Work lists of the matrix products, walked on the host: every tile, or every part of a divided one, is one workgroup's in one round, and a workgroup's list has no
+// gaps.  Grids of the planners over many sizes.  Host code only.
+#include <chrono>
+#include <cstdio>
+#include <cstdlib>
+#include <random>
+#include <vector>
+
+#include "wlb_dense.h"
+
+namespace wlb {
+int compute_units() { return 256; }
+}  // namespace wlb
+using namespace wlb;
+
+static long long grids = 0, divided = 0, items = 0;
+
+// lists that are walked item by item: larger ones would take minutes
+static bool walkable(const GemmGrid& g) { return (long long)g.ntm * g.ntn <= 20000; }
+
+static void walk(const GemmGrid& g, const char* what) {
+    const int tiles = g.ntm * g.ntn, steps = (g.depth + kStepK - 1) / kStepK;
+    ++grids;
+    divided += g.left > 0;
+    auto wrong = [&](const char* text, int a, int b) {
+        printf("%s: %s (%d, %d): %d x %d tiles, depth %d, %d workgroups, %d whole, %d in %d parts\n", what, text, a, b, g.ntm, g.ntn, g.depth, g.workgroups, g.whole, g.left, g.parts);
+        exit(1);
+    };
+    if (g.workgroups < kLists || g.workgroups % kLists || g.whole < 0 || g.left < 0 || g.parts < 1 || g.whole + g.left != tiles) wrong("grid", tiles, 0);
+    std::vector<int> covered(tiles, 0), places(g.left * g.parts, 0);
+    for (int b = 0; b < g.workgroups; ++b) {
+        GemmItem it;
+        int round = 0;
+        for (; g.item(b, round, it); ++round) {
+            ++items;
+            if (it.tm < 0 || it.tm >= g.ntm || it.tn < 0 || it.tn >= g.ntn) wrong("place", it.tm, it.tn);
+            if (it.part < 0) {
+                if (it.k0 != 0 || it.depth != g.depth) wrong("whole tile's depth", it.k0, it.depth);
+                covered[it.tn * g.ntm + it.tm] += std::max(steps, 1);
+            } else {
+                if (it.part >= g.left * g.parts) wrong("part", it.part, 0);
+                if (it.k0 % kStepK || it.k0 + it.depth > g.depth || it.depth < 0) wrong("part's depth", it.k0, it.depth);
+                // a tile's parts lie side by side, in the order of k
+                GemmItem tile;
+                g.place(g.whole + it.part / g.parts, tile);
+                if (tile.tm != it.tm || tile.tn != it.tn) wrong("tile of a part", it.part, it.tm);
+                if (it.k0 / kStepK != (int)((long long)steps * (it.part % g.parts) / g.parts)) wrong("order of parts", it.part, it.k0);
+                covered[it.tn * g.ntm + it.tm] += (it.depth + kStepK - 1) / kStepK;
+                ++places[it.part];
+            }
+        }
+        for (int later = 1; later <= 2; ++later)
+            if (g.item(b, round + later, it)) wrong("gap in the list of workgroup", b, round);
+    }
+    for (int t = 0; t < tiles; ++t)
+        if (covered[t] != std::max(steps, 1)) wrong("steps of a tile, instead of each once", covered[t], steps);
+    for (int p = 0; p < g.left * g.parts; ++p)
+        if (places[p] != 1) wrong("times that a part is computed", places[p], p);
+}
+
+static ProductArgs product(int pm, int qn, int depth, int twin = 0) {
+    ProductArgs a = {};
+    a.pm = pm; a.qn = qn; a.depth = depth; a.twin = twin;
+    return a;
+}
+
+static int groups[8] = {};
+
+// The gradients of an operator, as the calls plan them.
+static void gradients(int rows, int twin, int dx_pm, int dx_depth, std::vector<std::pair<int, int>> weights, const char* what) {
+    GroupArgs g = {};
+    g.n = 1;
+    if (dx_pm) g.a[0] = product(dx_pm, rows, dx_depth, twin);
+    for (auto& w : weights) g.a[g.n++] = product(w.first, w.second, rows);
+    const Group kind = plan_gradients(g);
+    ++groups[kind];
+    if (kind == kApart) return;
+    for (int k = 0; k < g.n; ++k)
+        if (g.a[k].qn && walkable(g.a[k].grid)) {
+            if (g.a[k].grid.workgroups != g.a[g.n - 1].grid.workgroups || g.turn[k] < 0 || g.turn[k] >= g.a[k].grid.workgroups / kLists) { printf("%s: launch\n", what); exit(1); }
+            if (g.a[k].grid.left && k != (rows <= kFewSlots ? 0 : g.n - 1)) { printf("%s: a product that no join follows is divided\n", what); exit(1); }
+            walk(g.a[k].grid, what);
+        }
+}
+static void linear_gradients(int n, int n_in, int n_out, bool act) {
+    const int twin = act && n <= kExactSlots ? n : 0, rows = twin ? 2 * n : n;
+    gradients(rows, twin, n_in, n_out, {{n_in, n_out}}, "gradients of a product");
+}
+static void ffn_gradients(int n, int hidden, int inner, int which) {
+    const int twin = n <= kExactSlots ? n : 0, rows = twin ? 2 * n : n;
+    std::vector<std::pair<int, int>> w;
+    if (which & 2) w.push_back({hidden, 2 * inner});
+    if (which & 4) w.push_back({inner, hidden});
+    gradients(rows, twin, which & 1 ? hidden : 0, 2 * inner, w, "gradients of a feed-forward block");
+}
+
+int main() {
+    std::mt19937 rng(5);
+    auto spread = [&](int lo, int hi) { return (int)std::exp(std::uniform_real_distribution<double>(std::log((double)lo), std::log(hi + 1.0))(rng)); };
+    auto width = [&](int hi) { return std::max(8, spread(8, hi) / 8 * 8); };
+
+    // sizes whose last product is divided in a group, with workgroups that have no whole tile in the last round
+    ffn_gradients(7680, 1024, 4096, 7);
+    ffn_gradients(5376, 1024, 4096, 7);
+    ffn_gradients(4096, 3080, 8192, 7);
+    ffn_gradients(7168, 4096, 14336, 7);
+    ffn_gradients(7691, 2624, 1328, 7);
+    ffn_gradients(5061, 152, 2600, 7);
+    linear_gradients(4189, 1544, 5000, true);
+    for (int i = 0; i < 3000; ++i) {
+        const int n = spread(1, 40000);
+        linear_gradients(n, width(16384), width(16384), i % 2);
+        ffn_gradients(n, width(8192), width(16384), 1 + rng() % 7);
+    }
+    for (int i = 0; i < 3000; ++i) {
+        const int pm = width(32768), qn = spread(1, 40000), depth = spread(1, 32768);
+        const Tiling t = best_tiling(pm, qn, depth, (int)(rng() % 3) * 6000);
+        if (walkable(t.grid)) walk(t.grid, "tiling");
+        const GemmGrid g = planned_grid((pm + 255) / 256, (qn + 255) / 256, depth, 256, kWideParts, kWideRounds);
+        const GemmGrid same((pm + 255) / 256, (qn + 255) / 256, depth, 256, kWideParts, kWideRounds);
+        if (g.whole != same.whole || g.left != same.left || g.parts != same.parts) { printf("the host's grid is not the device's\n"); return 1; }
+        if (walkable(g)) walk(g, "wide tiles");
+        long long cost = 0;
+        for (int most : {0, 256}) {
+            walk(narrow_grid(kTinyCost, pm, 64, depth, cost, true, most), "joined tiles");
+            walk(narrow_grid(kSmallCost, pm, 300, depth, cost, false, most), "narrow tiles");
+        }
+        walk(few_grid((pm + 127) / 128, depth), "few slots");
+        walk(joined_grid((pm + 127) / 128, depth, 256), "few slots, joined");
+    }
+    // any grid that a planner could come to
+    for (int i = 0; i < 20000; ++i) {
+        GemmGrid g;
+        g.ntm = spread(1, 60); g.ntn = spread(1, 60);
+        g.workgroups = kLists * spread(1, 64);
+        g.left = (int)(rng() % 2) * (int)(rng() % (g.ntm * g.ntn + 1));
+        g.whole = g.ntm * g.ntn - g.left;
+        g.parts = g.left ? spread(1, kMaxParts) : 1;
+        g.lead = (int)(rng() % (g.workgroups / kLists));
+        g.depth = spread(1, 20000);
+        walk(g, "any grid");
+    }
+    printf("work lists: ok: %lld grids, %lld divided, %lld items; gradients", grids, divided, items);
+    for (int k = 0; k < 8; ++k) printf(" %d", groups[k]);
+    printf("\n");
+    for (int k = 0; k < 8; ++k)
+        if (!groups[k]) { printf("a kind of launch that no size here has\n"); return 1; }
+    return 0;
+}
