@@ -60,7 +60,7 @@ struct GroupArgs {
 template <class S>
 long long plan_group(GroupArgs& g, const TileCost& cost) {
     const int per_cu = S::RING ? 1 : 2, workgroups = wide_workgroups() * per_cu, side = workgroups / kLists;
-    long long load[256] = {};
+    long long all = 0, load[256] = {};         // of every workgroup of an XCD, and beside that
     int at = 0;
     for (int k = 0; k < g.n; ++k) {
         ProductArgs& a = g.a[k];
@@ -84,7 +84,10 @@ long long plan_group(GroupArgs& g, const TileCost& cost) {
         }
         const int per = (a.grid.whole + kLists - 1) / kLists;
         g.turn[k] = at % side;
-        for (int i = 0; i < per; ++i) load[(at + i) % side] += (long long)steps * cost.step + cost.end;
+        // whole rounds, and one more tile from the workgroup `turn` on
+        const long long tile = (long long)steps * cost.step + cost.end;
+        all += per / side * tile;
+        for (int i = 0, n = per % side, w = g.turn[k]; i < n; ++i, w = w + 1 < side ? w + 1 : 0) load[w] += tile;
         at += per;
         if (part) {
             // An XCD's parts go to the workgroups that are done first of those where a product begins or ends: at equal loads behind the last whole tile, but where
@@ -100,10 +103,10 @@ long long plan_group(GroupArgs& g, const TileCost& cost) {
                     a.grid.lead = (from - end + side) % side;
                 }
             }
-            return std::max(*std::max_element(load, load + side), least + part) + join;
+            return all + std::max(*std::max_element(load, load + side), least + part) + join;
         }
     }
-    return *std::max_element(load, load + side);
+    return all + *std::max_element(load, load + side);
 }
 
 // How the products of a gradient, which wait for nothing of each other, are launched: one after the other, or in one launch of wide, small or tiny tiles; few slots' weights in

@@ -24,3 +24,9 @@ def test_every_tile_and_part_once(harness):
     run = subprocess.run([str(harness)], capture_output=True, text=True, timeout=300)
     assert run.returncode == 0, (run.stdout + run.stderr)[-4000:]
     assert "work lists: ok" in run.stdout
+
+
+def test_plan_of_the_largest_calls_is_short(harness):
+    """A call's host time does not grow with its tiles."""
+    run = subprocess.run([str(harness), "largest"], capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0, run.stdout + run.stderr

@@ -94,7 +94,50 @@ static void ffn_gradients(int n, int hidden, int inner, int which) {
     gradients(rows, twin, which & 1 ? hidden : 0, 2 * inner, w, "gradients of a feed-forward block");
 }
 
-int main() {
+// What plan_group says a group should take, against the time of every workgroup of an XCD added up tile by tile.
+template <class S>
+static void group_time(GroupArgs g, const TileCost& c) {
+    const long long said = plan_group<S>(g, c);
+    const int side = wide_workgroups() * (S::RING ? 1 : 2) / kLists;
+    std::vector<long long> load(side, 0);
+    long long most = 0, last = 0;
+    for (int k = 0; k < g.n; ++k) {
+        const GemmGrid& q = g.a[k].grid;
+        if (g.a[k].qn == 0) continue;
+        const long long steps = std::max(2, (q.depth + kStepK - 1) / kStepK), per = (q.whole + kLists - 1) / kLists;
+        for (long long i = 0; i < per; ++i) load[(g.turn[k] + i) % side] += steps * c.step + c.end;
+        most = *std::max_element(load.begin(), load.end());
+        if (q.left) {
+            const int parts = q.left * q.parts, share = (parts + kLists - 1) / kLists, from = g.turn[k] + (int)(per % side) + q.lead;
+            for (int i = 0; i < std::min(share, side); ++i) last = std::max(last, load[(from + i) % side]);
+            most = std::max(most, last + (steps + q.parts - 1) / q.parts * c.step + c.end) + kJoinLaunch + (long long)parts * c.join;
+        }
+    }
+    if (said != most) { printf("a group's time: %lld, tile by tile %lld\n", said, most); exit(1); }
+}
+static void group_times(int n, int hidden, int inner) {
+    GroupArgs g = {};
+    g.n = 3;
+    g.a[0] = product(hidden, n, 2 * inner); g.a[1] = product(hidden, 2 * inner, n); g.a[2] = product(inner, hidden, n);
+    group_time<Wide<true, true>>(g, kWideCost);
+    group_time<Small<true, true>>(g, kSmallCost);
+    group_time<Tiny<true, true>>(g, kTinyCost);
+}
+
+// The largest calls: a plan is a few divisions, whatever the number of tiles.
+static int largest() {
+    const auto start = std::chrono::steady_clock::now();
+    for (int k = 0; k < 10; ++k) {
+        linear_gradients(1990000, 1 << 20, 1 << 20, true);
+        ffn_gradients(1990000, 2040, 1 << 19, 7);
+    }
+    const double ms = std::chrono::duration<double, std::milli>(std::chrono::steady_clock::now() - start).count() / 20;
+    printf("plan of a largest call: %.4f ms\n", ms);
+    return ms < 5 ? 0 : 1;
+}
+
+int main(int argc, char** argv) {
+    if (argc > 1) return largest();
     std::mt19937 rng(5);
     auto spread = [&](int lo, int hi) { return (int)std::exp(std::uniform_real_distribution<double>(std::log((double)lo), std::log(hi + 1.0))(rng)); };
     auto width = [&](int hi) { return std::max(8, spread(8, hi) / 8 * 8); };
@@ -112,6 +155,7 @@ int main() {
         linear_gradients(n, width(16384), width(16384), i % 2);
         ffn_gradients(n, width(8192), width(16384), 1 + rng() % 7);
     }
+    for (int i = 0; i < 2000; ++i) group_times(spread(1, 20000), width(4096), width(8192));
     for (int i = 0; i < 3000; ++i) {
         const int pm = width(32768), qn = spread(1, 40000), depth = spread(1, 32768);
         const Tiling t = best_tiling(pm, qn, depth, (int)(rng() % 3) * 6000);
