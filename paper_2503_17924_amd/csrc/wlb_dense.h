@@ -28,12 +28,10 @@ struct ProductArgs {
 
 enum class Kinds { KK, MK, MM };     // of p and q
 
-// Launches the product (with an epilogue only where the kinds are KK).  a.parts: product_parts_bytes(a.qn) bytes.
+// Launches the product (with an epilogue only where the kinds are KK).  a.parts: parts_bytes_at_most(a.pm, a.qn, a.depth, a.twin) bytes, here and in a gradient.
 void launch_product(Kinds kinds, ProductArgs& a, hipStream_t stream);
 // Launches the products of a gradient that wait for nothing of each other: one of kinds MK (or null) and up to two of kinds MM, side by side where that pays.
 void launch_gradients(ProductArgs* dx, ProductArgs* const* dw, int n_dw, hipStream_t stream);
-// Bytes for the parts of divided tiles of products of n_rows slots, of up to `width` columns.
-size_t product_parts_bytes(int n_rows, int width);
 
 // Up to this many slots an operand that is rounded to bf16 has a second set of rows with what that leaves out: their few roundings find little to average out with, and
 // such products are bound by the weight's bytes.
@@ -44,6 +42,38 @@ __device__ __forceinline__ float rest_of(float v) {
 #pragma clang fp contract(off)          // of v as it was rounded, whichever product it came from: the same with what is kept and without
     const float rest = v - (float)(__bf16)v;
     return __builtin_isfinite(rest) ? rest : 0.f;
+}
+
+// ------------------------------------------------------------------------------------------
+// Plans.
+// What activations add to a wide tile's end, in ns, and rows in 32 bits with something beside them (4189 slots, 1544 x 5000, two rounds of wide tiles: 83 us plain, silu 87, gelu
+// 97; with a residual or slopes that are kept 12 more; 128 x 128 tiles 99 to 107).
+inline int activation_end(int act) { return act == WLB_ACT_GELU ? 6000 : act == WLB_ACT_SILU ? 2000 : 0; }
+constexpr int kRowsEnd = 6000;
+
+// The tiles that a product by itself should take least with.
+inline Tiling plan_product(Kinds kinds, const ProductArgs& a) {
+    const bool mp = kinds != Kinds::KK;
+    if (kinds != Kinds::MM && few_slots(mp, a.qn, a.pm, a.depth)) {
+        const int ntm = (a.pm + 127) / 128;
+        return Tiling{few_tiles(a.qn), a.twin ? joined_grid(ntm, a.depth, wide_workgroups()) : few_grid(ntm, a.depth), 0};
+    }
+    if (a.twin) {
+        Tiling t = {kTinyTiles, {}, 0};
+        t.grid = narrow_grid(kTinyCost, a.pm, a.qn, a.depth, t.cost, true);
+        return t;
+    }
+    return best_tiling(a.pm, a.qn, a.depth, activation_end(a.act) + (a.residual || a.kept ? kRowsEnd : 0));
+}
+// The same of the products that leave rows of h, dg and du: of those that have a second set of rows where there is one.
+inline Tiling plan_slots(Kinds kinds, int pm, int n_rows, int depth, int end) {
+    if (few_slots(kinds != Kinds::KK, n_rows, pm, depth)) return Tiling{few_tiles(n_rows), few_grid((pm + 127) / 128, depth), 0};
+    Tiling t = best_tiling(pm, n_rows, depth, end);
+    if (n_rows <= kExactSlots) {
+        t.kind = kTinyTiles;
+        t.grid = narrow_grid(kTinyCost, pm, n_rows, depth, t.cost);
+    }
+    return t;
 }
 
 // ------------------------------------------------------------------------------------------
@@ -109,9 +139,25 @@ long long plan_group(GroupArgs& g, const TileCost& cost) {
     return all + *std::max_element(load, load + side);
 }
 
+// Bytes for the parts of divided tiles in the calls of an operator, one product or launch after the other: y, dx and dW; (g, u), y, dh, dx, dW_in and dW_out.
+inline size_t linear_parts_bytes(int n_rows, int n_in, int n_out, int activation) {
+    const int dz = activation != WLB_ACT_NONE ? operand_rows(n_rows) : n_rows;
+    return std::max({parts_bytes_at_most(n_out, n_rows, n_in, false), parts_bytes_at_most(n_in, dz, n_out, dz > n_rows), parts_bytes_at_most(n_in, n_out, dz, false)});
+}
+inline size_t ffn_parts_bytes(int n_rows, int hidden, int inner) {
+    const int both = operand_rows(n_rows);
+    const bool joined = both > n_rows;
+    return std::max({parts_bytes_at_most(2 * inner, n_rows, hidden, false), parts_bytes_at_most(hidden, both, inner, joined), parts_bytes_at_most(inner, n_rows, hidden, false),
+                     parts_bytes_at_most(hidden, both, 2 * inner, joined), parts_bytes_at_most(hidden, 2 * inner, both, false), parts_bytes_at_most(inner, hidden, both, false)});
+}
+
 // How the products of a gradient, which wait for nothing of each other, are launched: one after the other, or in one launch of wide, small or tiny tiles; few slots' weights in
 // small tiles, dx in tiles of 128 columns and up to 32, 64 or 128 slots, or in tiny ones.
 enum Group { kApart, kWideGroup, kSmallGroup, kTinyGroup, kFewGroup32, kFewGroup64, kFewGroup128, kFewGroupTiny };
+inline int group_tiles(Group kind) {          // of the divided product
+    constexpr int kinds[] = {kWideTiles, kWideTiles, kSmallTiles, kTinyTiles, kFewTiles32, kFewTiles64, kFewTiles128, kTinyTiles};
+    return kinds[kind];
+}
 inline Group plan_gradients(GroupArgs& g) {
     const bool dx = g.a[0].qn > 0;
     const int rows = dx ? g.a[0].qn : g.n > 1 ? g.a[1].depth : 0;
@@ -238,10 +284,6 @@ __device__ __forceinline__ void activated(float z, float& value, float& slope) {
         slope = q + z * 0.3989422804014327f * e;
     }
 }
-// What they add to a wide tile's end, in ns, and rows in 32 bits with something beside them (4189 slots, 1544 x 5000, two rounds of wide tiles: 83 us plain, silu 87, gelu
-// 97; with a residual or slopes that are kept 12 more; 128 x 128 tiles 99 to 107).
-inline int activation_end(int act) { return act == WLB_ACT_GELU ? 6000 : act == WLB_ACT_SILU ? 2000 : 0; }
-constexpr int kRowsEnd = 6000;
 
 template <class F>
 __device__ __forceinline__ void with_activation(int act, F f) {

@@ -79,16 +79,6 @@ __device__ __forceinline__ bf16x4 gated(const f32x4& g, const f32x4& u, Piece& k
 // tiles that may have up to kExactSlots slots alone
 template <class S> constexpr bool kMayExact = S::TN <= kExactSlots || S::TM == 64;
 
-// The tiles that should take least, of those that have a second set of rows where there is one.
-static Tiling slots_tiling(int pm, int n_rows, int depth, int end) {
-    Tiling t = best_tiling(pm, n_rows, depth, end);
-    if (n_rows <= kExactSlots) {
-        t.kind = kTinyTiles;
-        t.grid = narrow_grid(kTinyCost, pm, n_rows, depth, t.cost);
-    }
-    return t;
-}
-
 // What the bytes that are kept add to a wide tile's end, and those that dg and du are made of and leave, in ns.
 constexpr int kKeptEnd = 8000, kInnerEnd = 20000;
 
@@ -217,19 +207,14 @@ static void launch_gate_tiles(GateArgs& a, hipStream_t stream) {
 template <int Act>
 static void launch_gate(GateArgs& a, hipStream_t stream) {
     if (a.n_rows == 0) return;
-    if (few_slots(false, a.n_rows, 2 * a.inner, a.hidden)) {
-        const int tile = slot_tile(a.n_rows);
-        a.grid = few_grid((a.inner + 63) / 64, a.hidden);
-        if (tile == 32) launch_gate_tiles<Few<2, false>, Act>(a, stream);
-        else if (tile == 64) launch_gate_tiles<Few<4, false>, Act>(a, stream);
-        else launch_gate_tiles<Few<8, false>, Act>(a, stream);
-        return;
-    }
-    const Tiling t = slots_tiling(2 * a.inner, a.n_rows, a.hidden, activation_end(Act) / 2 + (a.to.values ? kKeptEnd : 0));
+    const Tiling t = plan_slots(Kinds::KK, 2 * a.inner, a.n_rows, a.hidden, activation_end(Act) / 2 + (a.to.values ? kKeptEnd : 0));
     a.grid = t.grid;
     if (t.kind == kWideTiles) launch_gate_tiles<Wide<false, false>, Act>(a, stream);
     else if (t.kind == kSmallTiles) launch_gate_tiles<Small<false, false>, Act>(a, stream);
-    else launch_gate_tiles<Tiny<false, false>, Act>(a, stream);
+    else if (t.kind == kTinyTiles) launch_gate_tiles<Tiny<false, false>, Act>(a, stream);
+    else if (t.kind == kFewTiles32) launch_gate_tiles<Few<2, false>, Act>(a, stream);
+    else if (t.kind == kFewTiles64) launch_gate_tiles<Few<4, false>, Act>(a, stream);
+    else launch_gate_tiles<Few<8, false>, Act>(a, stream);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -356,19 +341,14 @@ static void launch_inner_tiles(InnerArgs& a, hipStream_t stream) {
 }
 static void launch_inner(InnerArgs& a, hipStream_t stream) {
     if (a.n_rows == 0) return;
-    if (few_slots(true, a.n_rows, a.inner, a.hidden)) {
-        const int tile = slot_tile(a.n_rows);
-        a.grid = few_grid((a.inner + 127) / 128, a.hidden);
-        if (tile == 32) launch_inner_tiles<Few<2, true>>(a, stream);
-        else if (tile == 64) launch_inner_tiles<Few<4, true>>(a, stream);
-        else launch_inner_tiles<Few<8, true>>(a, stream);
-        return;
-    }
-    const Tiling t = slots_tiling(a.inner, a.n_rows, a.hidden, kInnerEnd);
+    const Tiling t = plan_slots(Kinds::MK, a.inner, a.n_rows, a.hidden, kInnerEnd);
     a.grid = t.grid;
     if (t.kind == kWideTiles) launch_inner_tiles<Wide<true, false>>(a, stream);
     else if (t.kind == kSmallTiles) launch_inner_tiles<Small<true, false>>(a, stream);
-    else launch_inner_tiles<Tiny<true, false>>(a, stream);
+    else if (t.kind == kTinyTiles) launch_inner_tiles<Tiny<true, false>>(a, stream);
+    else if (t.kind == kFewTiles32) launch_inner_tiles<Few<2, true>>(a, stream);
+    else if (t.kind == kFewTiles64) launch_inner_tiles<Few<4, true>>(a, stream);
+    else launch_inner_tiles<Few<8, true>>(a, stream);
 }
 
 static void launch_gate(int act, GateArgs& a, hipStream_t stream) {
@@ -397,7 +377,7 @@ static FfnLayout ffn_layout(const wlb_ffn_desc& d) {
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
     const bool gaps = d.n_rows < d.n_q;
-    L.off_parts = take(product_parts_bytes(d.n_rows, std::max(2 * d.inner, d.hidden)));
+    L.off_parts = take(std::max<size_t>(1, ffn_parts_bytes(d.n_rows, d.hidden, d.inner)));          // a workspace of no bytes would have no address
     L.off_x = take(gaps ? 2 * n * h : 0);
     L.off_h = at;                    // where nothing is kept
     L.fwd_bytes = at + align_up(2 * operand * f, 256);

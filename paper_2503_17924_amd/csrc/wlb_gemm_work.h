@@ -230,7 +230,7 @@ inline long long wide_cost(const TileCost& c, const GemmGrid& g) {
 }
 // Which tiles a product should take least with.  end: what a wide tile's end takes beyond a plain one's, in ns; the others' ends, of a quarter and a sixteenth of the values, run
 // beside another workgroup's steps.
-enum { kWideTiles, kSmallTiles, kTinyTiles };
+enum { kWideTiles, kSmallTiles, kTinyTiles, kFewTiles32, kFewTiles64, kFewTiles128 };
 struct Tiling { int kind; GemmGrid grid; long long cost; };
 inline Tiling best_tiling(int pm, int qn, int depth, int end = 0) {
     TileCost wide = kWideCost, narrow[2] = {kSmallCost, kTinyCost};
@@ -264,5 +264,27 @@ inline GemmGrid joined_grid(int ntm, int depth, int workgroups) {
         g.parts = 1;
     }
     return g;
+}
+inline int few_tiles(int n_rows) { return n_rows <= 32 ? kFewTiles32 : n_rows <= 64 ? kFewTiles64 : kFewTiles128; }
+
+// Bytes of the parts of a product's divided tiles.
+inline size_t tile_bytes(int kind) {
+    constexpr int values[] = {256 * 256, 128 * 128, 64 * 64, 128 * 32, 128 * 64, 128 * 128};
+    return sizeof(float) * values[kind];
+}
+inline size_t parts_bytes(int kind, const GemmGrid& g) { return tile_bytes(kind) * (size_t)g.left * g.parts; }
+// At most as many as any of the plans above has, for a product by itself or in a group: a launch of parts, and no part of fewer steps than each has at least.
+// joined: in narrow tiles all of them are in parts, of which there may be but one.
+inline size_t parts_bytes_at_most(int pm, int qn, int depth, bool joined) {
+    const long long steps = std::max(2, (depth + kStepK - 1) / kStepK), cus = wide_workgroups();
+    auto items = [](long long tiles, long long parts, long long most, bool all) { return (size_t)std::max(parts < 2 ? 0 : std::min(most, tiles * parts), all ? tiles : 0); };
+    auto tiles = [&](int tm, int tn) { return (long long)((pm + tm - 1) / tm) * ((qn + tn - 1) / tn); };
+    const long long wide = tiles(256, 256), wide_parts = steps / kWideParts, narrow_parts = steps / kNarrowSteps;
+    // by itself up to kWideRounds rounds of the tiles that are left behind whole rounds, in a group one
+    size_t bytes = tile_bytes(kWideTiles) * std::max(items(wide % cus, wide_parts, kWideRounds * cus, false), items(wide, wide_parts, cus, false));
+    bytes = std::max(bytes, tile_bytes(kSmallTiles) * items(tiles(128, 128), narrow_parts, 2 * cus, false));
+    bytes = std::max(bytes, tile_bytes(kTinyTiles) * items(tiles(64, 64), narrow_parts, 2 * cus, joined));
+    if (qn <= kFewSlots) bytes = std::max(bytes, tile_bytes(few_tiles(qn)) * items((pm + 127) / 128, steps / kFewParts, cus, joined));
+    return bytes;
 }
 }  // namespace wlb

@@ -153,13 +153,6 @@ __global__ void __launch_bounds__(256) product_join_kernel(ProductArgs a) {
     join_any<S>(w, a.parts, join, a.twin);
 }
 
-size_t product_parts_bytes(int n_rows, int width) {
-    // a gradient of a weight has wide tiles from kStepK rows on, whatever the tiles of the slots are, and small ones, two to a workgroup of these, below that
-    const int tile = n_rows > kStepK ? 256 : slot_tile(n_rows);
-    const size_t bytes = std::max(sizeof(float) * 256 * (size_t)tile * wide_workgroups() * (tile < 256 ? 1 : kWideRounds), sizeof(float) * 128 * 128 * 2 * (size_t)wide_workgroups());
-    return n_rows <= kExactSlots ? std::max(bytes, sizeof(float) * 64 * align_up(width, 128)) : bytes;
-}
-
 template <class S, int Epilogue, int Act>
 static void launch_one(ProductArgs& a, hipStream_t stream) {
     product_kernel<S, Epilogue, Act><<<a.grid.workgroups, 256, 0, stream>>>(a);
@@ -182,43 +175,26 @@ static void launch_epilogue(ProductArgs& a, hipStream_t stream) {
     else if (a.bias || a.residual) launch_activated<S, WLB_ACT_NONE>(a, stream);
     else launch_one<S, kPlain, WLB_ACT_NONE>(a, stream);
 }
-template <class S>
-static void launch_few(ProductArgs& a, hipStream_t stream) {
-    a.grid = a.twin ? joined_grid((a.pm + S::TM - 1) / S::TM, a.depth, wide_workgroups()) : few_grid((a.pm + S::TM - 1) / S::TM, a.depth);
-    launch_epilogue<S>(a, stream);
-}
-// The tiles that should take least.
 template <bool MP, bool MQ>
-static void launch_many(ProductArgs& a, hipStream_t stream) {
-    if (a.twin) {
-        long long unused = 0;
-        a.grid = narrow_grid(kTinyCost, a.pm, a.qn, a.depth, unused, true);
-        return launch_epilogue<Tiny<MP, MQ>>(a, stream);
+static void launch_tiles(int kind, ProductArgs& a, hipStream_t stream) {
+    if (kind == kWideTiles) launch_epilogue<Wide<MP, MQ>>(a, stream);
+    else if (kind == kSmallTiles) launch_epilogue<Small<MP, MQ>>(a, stream);
+    else if (kind == kTinyTiles) launch_epilogue<Tiny<MP, MQ>>(a, stream);
+    if constexpr (!MQ) {
+        if (kind == kFewTiles32) launch_epilogue<Few<2, MP>>(a, stream);
+        else if (kind == kFewTiles64) launch_epilogue<Few<4, MP>>(a, stream);
+        else if (kind == kFewTiles128) launch_epilogue<Few<8, MP>>(a, stream);
     }
-    const Tiling t = best_tiling(a.pm, a.qn, a.depth, activation_end(a.act) + (a.residual || a.kept ? kRowsEnd : 0));
-    a.grid = t.grid;
-    if (t.kind == kWideTiles) launch_epilogue<Wide<MP, MQ>>(a, stream);
-    else if (t.kind == kSmallTiles) launch_epilogue<Small<MP, MQ>>(a, stream);
-    else launch_epilogue<Tiny<MP, MQ>>(a, stream);
 }
 
 void launch_product(Kinds kinds, ProductArgs& a, hipStream_t stream) {
     if (a.qn == 0 || a.pm == 0) return;
     if (!a.to) a.out_limit = a.twin ? a.twin : a.qn;
-    const int tile = kinds != Kinds::MM && few_slots(kinds == Kinds::MK, a.qn, a.pm, a.depth) ? slot_tile(a.qn) : 256;
-    if (kinds == Kinds::KK) {
-        if (tile == 32) launch_few<Few<2, false>>(a, stream);
-        else if (tile == 64) launch_few<Few<4, false>>(a, stream);
-        else if (tile == 128) launch_few<Few<8, false>>(a, stream);
-        else launch_many<false, false>(a, stream);
-    } else if (kinds == Kinds::MK) {
-        if (tile == 32) launch_few<Few<2, true>>(a, stream);
-        else if (tile == 64) launch_few<Few<4, true>>(a, stream);
-        else if (tile == 128) launch_few<Few<8, true>>(a, stream);
-        else launch_many<true, false>(a, stream);
-    } else {
-        launch_many<true, true>(a, stream);
-    }
+    const Tiling t = plan_product(kinds, a);
+    a.grid = t.grid;
+    if (kinds == Kinds::KK) launch_tiles<false, false>(t.kind, a, stream);
+    else if (kinds == Kinds::MK) launch_tiles<true, false>(t.kind, a, stream);
+    else launch_tiles<true, true>(t.kind, a, stream);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -440,7 +416,7 @@ static LinearLayout linear_layout(const wlb_linear_desc& d) {
     const size_t n = d.n_rows, out = d.n_out;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
-    L.off_parts = take(product_parts_bytes(d.n_rows, std::max(d.n_in, d.n_out)));
+    L.off_parts = take(std::max<size_t>(1, linear_parts_bytes(d.n_rows, d.n_in, d.n_out, d.activation)));          // a workspace of no bytes would have no address
     const bool gaps = d.n_rows < d.n_q;
     L.off_x = take(gaps ? 2 * n * d.n_in : 0);
     L.fwd_bytes = at;

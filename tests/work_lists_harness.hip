@@ -1,5 +1,5 @@
 // Work lists of the matrix products, walked on the host: every tile, or every part of a divided one, is one workgroup's in one round, and a workgroup's list has no
-// gaps.  Grids of the planners over many sizes.  Host code only.
+// gaps.  Grids of the planners over many sizes, and the room that their parts take.  Host code only.
 #include <chrono>
 #include <cstdio>
 #include <cstdlib>
@@ -8,8 +8,9 @@
 
 #include "wlb_dense.h"
 
+static int cus = 256;
 namespace wlb {
-int compute_units() { return 256; }
+int compute_units() { return cus; }
 }  // namespace wlb
 using namespace wlb;
 
@@ -64,7 +65,26 @@ static ProductArgs product(int pm, int qn, int depth, int twin = 0) {
     return a;
 }
 
-static int groups[8] = {};
+static int groups[8] = {}, tiles[6] = {};
+static size_t room = 0, largest_need = 0;         // bytes for parts in the calls of the operator that is looked at, and what its plans took most
+
+static void takes(int kind, const GemmGrid& g, const char* what) {
+    const size_t need = parts_bytes(kind, g);
+    largest_need = std::max(largest_need, need);
+    if (need > room) { printf("%s: parts of %zu bytes, room for %zu\n", what, need, room); exit(1); }
+}
+static void alone(Kinds kinds, const ProductArgs& a, const char* what) {
+    const Tiling t = plan_product(kinds, a);
+    ++tiles[t.kind];
+    takes(t.kind, t.grid, what);
+    if (walkable(t.grid)) walk(t.grid, what);
+}
+static void slots(Kinds kinds, int pm, int rows, int depth, int end, const char* what) {
+    const Tiling t = plan_slots(kinds, pm, rows, depth, end);
+    ++tiles[t.kind];
+    takes(t.kind, t.grid, what);
+    if (walkable(t.grid)) walk(t.grid, what);
+}
 
 // The gradients of an operator, as the calls plan them.
 static void gradients(int rows, int twin, int dx_pm, int dx_depth, std::vector<std::pair<int, int>> weights, const char* what) {
@@ -74,7 +94,12 @@ static void gradients(int rows, int twin, int dx_pm, int dx_depth, std::vector<s
     for (auto& w : weights) g.a[g.n++] = product(w.first, w.second, rows);
     const Group kind = plan_gradients(g);
     ++groups[kind];
-    if (kind == kApart) return;
+    if (kind == kApart) {
+        if (dx_pm) alone(Kinds::MK, g.a[0], what);
+        for (int k = 1; k < g.n; ++k) alone(Kinds::MM, g.a[k], what);
+        return;
+    }
+    for (int k = 0; k < g.n; ++k) takes(group_tiles(kind), g.a[k].grid, what);
     for (int k = 0; k < g.n; ++k)
         if (g.a[k].qn && walkable(g.a[k].grid)) {
             if (g.a[k].grid.workgroups != g.a[g.n - 1].grid.workgroups || g.turn[k] < 0 || g.turn[k] >= g.a[k].grid.workgroups / kLists) { printf("%s: launch\n", what); exit(1); }
@@ -82,16 +107,38 @@ static void gradients(int rows, int twin, int dx_pm, int dx_depth, std::vector<s
             walk(g.a[k].grid, what);
         }
 }
-static void linear_gradients(int n, int n_in, int n_out, bool act) {
+// All launches of an operator's calls, with any of their outputs left out.
+static void linear(int n, int n_in, int n_out, int act) {
     const int twin = act && n <= kExactSlots ? n : 0, rows = twin ? 2 * n : n;
+    room = linear_parts_bytes(n, n_in, n_out, act);
+    largest_need = 0;
+    ProductArgs y = product(n_out, n, n_in);
+    y.act = act;
+    alone(Kinds::KK, y, "product");
+    __bf16 some;
+    y.residual = &some;
+    alone(Kinds::KK, y, "product with a residual");
     gradients(rows, twin, n_in, n_out, {{n_in, n_out}}, "gradients of a product");
+    gradients(rows, twin, n_in, n_out, {}, "gradient of x");
+    gradients(rows, twin, 0, 0, {{n_in, n_out}}, "gradient of the weight");
 }
-static void ffn_gradients(int n, int hidden, int inner, int which) {
+static void ffn(int n, int hidden, int inner, int act) {
     const int twin = n <= kExactSlots ? n : 0, rows = twin ? 2 * n : n;
-    std::vector<std::pair<int, int>> w;
-    if (which & 2) w.push_back({hidden, 2 * inner});
-    if (which & 4) w.push_back({inner, hidden});
-    gradients(rows, twin, which & 1 ? hidden : 0, 2 * inner, w, "gradients of a feed-forward block");
+    room = ffn_parts_bytes(n, hidden, inner);
+    largest_need = 0;
+    for (int end : {0, 2000, 8000, 11000}) slots(Kinds::KK, 2 * inner, n, hidden, end, "gate");
+    ProductArgs y = product(hidden, rows, inner, twin);
+    alone(Kinds::KK, y, "product with Wd");
+    __bf16 some;
+    y.residual = &some;
+    alone(Kinds::KK, y, "product with Wd and a residual");
+    slots(Kinds::MK, inner, n, hidden, 20000, "inner gradient");
+    for (int which = 1; which < 8; ++which) {
+        std::vector<std::pair<int, int>> w;
+        if (which & 2) w.push_back({hidden, 2 * inner});
+        if (which & 4) w.push_back({inner, hidden});
+        gradients(rows, twin, which & 1 ? hidden : 0, 2 * inner, w, "gradients of a feed-forward block");
+    }
 }
 
 // What plan_group says a group should take, against the time of every workgroup of an XCD added up tile by tile.
@@ -128,8 +175,8 @@ static void group_times(int n, int hidden, int inner) {
 static int largest() {
     const auto start = std::chrono::steady_clock::now();
     for (int k = 0; k < 10; ++k) {
-        linear_gradients(1990000, 1 << 20, 1 << 20, true);
-        ffn_gradients(1990000, 2040, 1 << 19, 7);
+        linear(1990000, 1 << 20, 1 << 20, true);
+        ffn(1990000, 2040, 1 << 19, 7);
     }
     const double ms = std::chrono::duration<double, std::milli>(std::chrono::steady_clock::now() - start).count() / 20;
     printf("plan of a largest call: %.4f ms\n", ms);
@@ -143,18 +190,23 @@ int main(int argc, char** argv) {
     auto width = [&](int hi) { return std::max(8, spread(8, hi) / 8 * 8); };
 
     // sizes whose last product is divided in a group, with workgroups that have no whole tile in the last round
-    ffn_gradients(7680, 1024, 4096, 7);
-    ffn_gradients(5376, 1024, 4096, 7);
-    ffn_gradients(4096, 3080, 8192, 7);
-    ffn_gradients(7168, 4096, 14336, 7);
-    ffn_gradients(7691, 2624, 1328, 7);
-    ffn_gradients(5061, 152, 2600, 7);
-    linear_gradients(4189, 1544, 5000, true);
+    ffn(7680, 1024, 4096, 2);
+    ffn(5376, 1024, 4096, 2);
+    ffn(4096, 3080, 8192, 2);
+    ffn(7168, 4096, 14336, 2);
+    ffn(7691, 2624, 1328, 2);
+    ffn(5061, 152, 2600, 2);
+    linear(4189, 1544, 5000, 3);
+    int full = 0;
     for (int i = 0; i < 3000; ++i) {
-        const int n = spread(1, 40000);
-        linear_gradients(n, width(16384), width(16384), i % 2);
-        ffn_gradients(n, width(8192), width(16384), 1 + rng() % 7);
+        cus = i % 8 == 6 ? 32 : i % 8 == 7 ? 304 : 256;
+        const int n = spread(1, i % 3 ? 40000 : 200);
+        linear(n, width(16384), width(16384), i % 4);
+        full += largest_need == room;
+        ffn(n, width(8192), width(16384), 2);
+        full += largest_need == room;
     }
+    cus = 256;
     for (int i = 0; i < 2000; ++i) group_times(spread(1, 20000), width(4096), width(8192));
     for (int i = 0; i < 3000; ++i) {
         const int pm = width(32768), qn = spread(1, 40000), depth = spread(1, 32768);
@@ -184,7 +236,14 @@ int main(int argc, char** argv) {
         g.depth = spread(1, 20000);
         walk(g, "any grid");
     }
-    printf("work lists: ok: %lld grids, %lld divided, %lld items; gradients", grids, divided, items);
+    for (int k = 0; k < 6; ++k)
+        if (!tiles[k]) { printf("tiles that no size here has: %d\n", k); return 1; }
+    // small calls take little: 65 slots, 1024 x 1024, 2 MiB of parts, one of 64 x 64 its own tiles alone
+    if (linear_parts_bytes(65, 1024, 1024, 0) > 4u << 20 || linear_parts_bytes(1, 64, 64, 0) > 0 || ffn_parts_bytes(1, 64, 64) > 64u << 10) {
+        printf("room of small calls: %zu %zu %zu\n", linear_parts_bytes(65, 1024, 1024, 0), linear_parts_bytes(1, 64, 64, 0), ffn_parts_bytes(1, 64, 64));
+        return 1;
+    }
+    printf("room taken as a whole: %d of 6000; work lists: ok: %lld grids, %lld divided, %lld items; gradients", full, grids, divided, items);
     for (int k = 0; k < 8; ++k) printf(" %d", groups[k]);
     printf("\n");
     for (int k = 0; k < 8; ++k)
