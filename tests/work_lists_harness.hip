@@ -1,8 +1,8 @@
 // Work lists of the matrix products, walked on the host: every tile, or every part of a divided one, is one workgroup's in one round, and a workgroup's list has no
 // gaps.  Grids of the planners over many sizes, and the room that their parts take.  Host code only.
-#include <chrono>
 #include <cstdio>
 #include <cstdlib>
+#include <ctime>
 #include <random>
 #include <vector>
 
@@ -16,8 +16,9 @@ using namespace wlb;
 
 static long long grids = 0, divided = 0, items = 0;
 
-// lists that are walked item by item: larger ones would take minutes
-static bool walkable(const GemmGrid& g) { return (long long)g.ntm * g.ntn <= 20000; }
+// lists that are walked item by item: larger ones would take minutes, and none is where plans are timed
+static bool walking = true;
+static bool walkable(const GemmGrid& g) { return walking && (long long)g.ntm * g.ntn <= 20000; }
 
 static void walk(const GemmGrid& g, const char* what) {
     const int tiles = g.ntm * g.ntn, steps = (g.depth + kStepK - 1) / kStepK;
@@ -173,13 +174,14 @@ static void group_times(int n, int hidden, int inner) {
 
 // The largest calls: a plan is a few divisions, whatever the number of tiles.
 static int largest() {
-    const auto start = std::chrono::steady_clock::now();
+    walking = false;
+    const clock_t start = clock();
     for (int k = 0; k < 10; ++k) {
         linear(1990000, 1 << 20, 1 << 20, true);
         ffn(1990000, 2040, 1 << 19, 7);
     }
-    const double ms = std::chrono::duration<double, std::milli>(std::chrono::steady_clock::now() - start).count() / 20;
-    printf("plan of a largest call: %.4f ms\n", ms);
+    const double ms = 1e3 * (double)(clock() - start) / CLOCKS_PER_SEC / 20;
+    printf("plans of a largest call, with any of its outputs left out: %.4f ms\n", ms);
     return ms < 5 ? 0 : 1;
 }
 
